@@ -349,6 +349,55 @@ int moe_combine(moe_plan_t* plan, const void* d_rows, const int32_t* d_slot_of,
 int moe_layer(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* d_bias,
               const void* d_wg, const void* d_wu, const void* d_wd, void* d_y, void* stream);
 
+/* The whole layer for a few tokens in ONE kernel launch (decoding): what moe_layer computes, for T <= MOE_FEW_MAX_TOKENS
+ * (MOE_ERR_UNSUPPORTED beyond), bounded by reading the picked experts' weights once.  Arguments as for moe_layer; of the plan's
+ * configuration T, H, E, K, F, dtype, renormalize and wait_limit_ns count (tp_shards changes nothing: an expert is computed
+ * whole), identity experts are refused (MOE_ERR_ARG).  It differs from moe_layer in its rounding: logits are fp32 sums in an
+ * order of their own (not the ascending chain of moe_route, so the pick between two experts whose logits agree to fp32 rounding
+ * may differ), and an expert's output is not rounded to dtype before it is weighted and added.  The result does not depend on
+ * the order in which the CTAs run.  moe_layer_buffer 0, 1 and 3 (picks, their weights, rows per expert) hold the call's values
+ * behind it, the other buffers anything.
+ * The launch is cooperative (all its CTAs are resident; one per SM): it starts when the SMs have room for all of it.  Its CTAs
+ * wait for one another, each wait bounded by wait_limit_ns (0 = 2 s); on expiry the status word reads MOE_ERR_TIMEOUT and y holds
+ * anything.  The plan's device has to be the current one (MOE_ERR_ARG). */
+#define MOE_FEW_MAX_TOKENS 16
+int moe_layer_few(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* d_bias,
+                  const void* d_wg, const void* d_wu, const void* d_wd, void* d_y, void* stream);
+
+/* 4-bit weights with group scales: `experts` matrices [N, C] in groups of `group` (32, 64 or 128, dividing C) columns,
+ *   W[e,n,c] = scales[e, c/group, n] * (code(e,n,c) - 8),   code 0..15.
+ * codes: [experts, N, C/2] bytes; the eight columns c..c+7 (c a multiple of 8) are one little-endian 32-bit word, whose
+ * nibbles hold, from the least significant one on, columns c, c+2, c+4, c+6, c+1, c+3, c+5, c+7.
+ * scales: [experts, C/group, N] bf16.  Both in DEVICE memory, 16-byte aligned. */
+typedef struct {
+  void* codes;
+  void* scales;
+} moe_w4_t;
+
+/* moe_layer_few with 4-bit expert weights: wg, wu as [E] matrices [F, H], wd as [E] matrices [H, F], one group size for the three.
+ * (The structs are read before the call returns.)  x, the router weight and y are bf16 (a plan of dtype fp32 is refused with
+ * MOE_ERR_UNSUPPORTED, so is another group size; MOE_ERR_ARG where the group does not divide H and F).  Products are formed with the
+ * exact integers code - 8 and summed in fp32, a group's sum is scaled once. */
+int moe_layer_few_w4(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* d_bias, int32_t group,
+                     const moe_w4_t* wg, const moe_w4_t* wu, const moe_w4_t* wd, void* d_y, void* stream);
+
+/* Products of a few rows with 4-bit matrices: y[m,:] = W[d_expert[m]] x[m,:], m < M, fp32 sums, rounded once.
+ * in: d_x [M,C] bf16, d_expert [M] int32 (NULL with experts == 1: that matrix for every row).  out: d_y [M,N] bf16.
+ * A row whose id is outside [0, experts) is skipped: its y keeps its old contents.  Rows with the same matrix share its reading as
+ * far as they are among the same MOE_FEW_MAX_TOKENS consecutive rows; M may be any number (with hundreds of rows
+ * moe_w4_unpack and a matrix product are the better way).  Needs no plan and no workspace; runs on the current device. */
+int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const moe_w4_t* w, int32_t M, const void* d_x,
+                  const int32_t* d_expert, void* d_y, void* stream);
+
+/* bf16 or fp32 weights (dtype) d_w [experts, N, C] into 4 bits: scale = amax / 7 over the group (divided in fp32, rounded to bf16),
+ * code = clamp(round(w / scale), -8, 7) + 8, decided on the exact quotient, ties to even.  A group of zeros (or one whose scale rounds to zero) gets scale
+ * 0 and codes 8; one that holds a NaN or an infinity gets scale NaN, so that every product with it is NaN. */
+int moe_w4_pack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t group, const void* d_w, const moe_w4_t* out, void* stream);
+
+/* The weights that the codes stand for, scale * (code - 8) rounded to dtype, d_out [experts, N, C]: what moe_layer and
+ * moe_expert_ffn take for a prefill on 4-bit weights. */
+int moe_w4_unpack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t group, const moe_w4_t* w, void* d_out, void* stream);
+
 /* The whole layer with the activations in HOST memory: copies h_x [T,H] to the device,
  * runs moe_layer, copies y back to h_y [T,H] and synchronises the stream.  Weights stay
  * device-resident (they are parameters, not per-step inputs).  Pinned host memory makes the

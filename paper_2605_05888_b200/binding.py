@@ -6,6 +6,7 @@ missing or no CUDA device is present, calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -22,7 +23,7 @@ TILE_ROWS = 128
 STAGES = ["route", "dispatch", "worklist", "gemm1", "gemm2", "combine"]
 
 EXPORTS = ["moe_dispatch_noalloc", "moe_dispatch_ep", "moe_ep_tiles", "moe_combine_ep", "moe_pool_tiles", "moe_workspace_bytes", "moe_plan_create", "moe_plan_destroy", "moe_route",
-           "moe_dispatch", "moe_expert_ffn", "moe_expert_ffn_push", "moe_combine", "moe_combine_staged", "moe_layer", "moe_layer_host", "moe_layer_host_submit", "moe_layer_host_wait", "moe_layer_timed",
+           "moe_dispatch", "moe_expert_ffn", "moe_expert_ffn_push", "moe_combine", "moe_combine_staged", "moe_layer", "moe_layer_few", "moe_layer_few_w4", "moe_w4_matvec", "moe_w4_pack", "moe_w4_unpack", "moe_layer_host", "moe_layer_host_submit", "moe_layer_host_wait", "moe_layer_timed",
            "moe_layer_buffer", "moe_availability_trace",
            "moe_ffn_clock_mhz", "moe_last_launch_count", "moe_last_status", "moe_last_cuda_error", "moe_strerror"]
 
@@ -42,6 +43,36 @@ class EpPeer(ctypes.Structure):
     """moe_ep_peer_t: one rank's receive buffers as device pointers valid on the calling GPU."""
     _fields_ = [("recv", ctypes.c_void_p), ("row_pointer", ctypes.c_void_p), ("tile_count", ctypes.c_void_p),
                 ("src_info", ctypes.c_void_p), ("rows_done", ctypes.c_void_p)]
+
+
+class W4T(ctypes.Structure):
+    """moe_w4_t: device pointers of 4-bit matrices' codes and scales."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class W4:
+    """4-bit matrices [experts, N, C]: codes uint8 [experts, N, C/2], scales bf16 [experts, C/group, N] (or both without the
+    first axis: one matrix).  Keeps the tensors alive; W4.empty allocates them for moe_w4_pack."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16 or codes.dim() != scales.dim() or codes.dim() not in (2, 3):
+            raise ValueError("codes are uint8 [experts, N, C/2], scales bf16 [experts, C/group, N]")
+        lead = codes.shape[:-2]
+        self.experts, self.N, self.C = (lead[0] if lead else 1), codes.shape[-2], codes.shape[-1] * 2
+        if scales.shape[:-2] != lead or scales.shape[-1] != self.N or scales.shape[-2] == 0 or self.C % scales.shape[-2] != 0:
+            raise ValueError(f"codes {tuple(codes.shape)} and scales {tuple(scales.shape)} do not belong together")
+        if codes.device != scales.device:
+            raise ValueError("codes and scales are on different devices")
+        self.group = self.C // scales.shape[-2]
+        self.codes, self.scales = codes, scales
+        self.struct = W4T(_ptr(codes), _ptr(scales))
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, N: int, C: int, group: int, experts: int | None = None, device="cuda") -> "W4":
+        lead = () if experts is None else (experts,)
+        return cls(torch.empty(*lead, N, C // 2, dtype=torch.uint8, device=device),
+                   torch.empty(*lead, C // group, N, dtype=torch.bfloat16, device=device))
 
 
 class MoeError(RuntimeError):
@@ -74,6 +105,12 @@ def lib() -> ctypes.CDLL:
         L.moe_expert_ffn_push.argtypes = [vp, vp, i32p, i32p, vp, vp, vp, vp, i32p, i32p, vp]
         L.moe_combine_staged.argtypes = [vp, vp, i32p, fp, vp, vp]
         L.moe_layer.argtypes = [vp] * 9
+        L.moe_layer_few.argtypes = [vp] * 9
+        w4p, i32 = ctypes.POINTER(W4T), ctypes.c_int32
+        L.moe_layer_few_w4.argtypes = [vp, vp, vp, fp, i32, w4p, w4p, w4p, vp, vp]
+        L.moe_w4_matvec.argtypes = [i32, i32, i32, i32, w4p, i32, vp, i32p, vp, vp]
+        L.moe_w4_pack.argtypes = [i32, i32, i32, i32, i32, vp, w4p, vp]
+        L.moe_w4_unpack.argtypes = [i32, i32, i32, i32, i32, w4p, vp, vp]
         L.moe_layer_host.argtypes = [vp] * 9
         L.moe_layer_host_submit.argtypes = [vp] * 9 + [ctypes.POINTER(ctypes.c_int64)]
         L.moe_layer_host_wait.argtypes = [vp, ctypes.c_int64]
@@ -174,6 +211,49 @@ def moe_combine_ep(cfg: MoeConfig, staging, rows_back, cap_rows: int, out_rows, 
                                 _ptr(status), _stream(stream)), "moe_combine_ep")
 
 
+def _on_device_of(t: torch.Tensor):
+    """The calls that take no plan run on the current device: make it the tensors' one."""
+    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"fp32 or bf16, not {t.dtype}")
+    return DTYPE_FP32 if t.dtype == torch.float32 else DTYPE_BF16
+
+
+def _w4_shape(w: W4, t: torch.Tensor) -> None:
+    if t.numel() != w.experts * w.N * w.C or t.shape[-2:] != (w.N, w.C) or t.device != w.codes.device:
+        raise ValueError(f"weights {tuple(t.shape)} on {t.device} are not what codes {tuple(w.codes.shape)} on {w.codes.device} stand for")
+
+
+def moe_w4_matvec(w: W4, x, expert, y, stream=None) -> None:
+    """y[m] = W[expert[m]] x[m] on 4-bit matrices; expert None: one matrix for every row.  x [M, C], y [M, N] bf16."""
+    M = x.shape[0]
+    if x.dtype != torch.bfloat16 or y.dtype != torch.bfloat16 or x.shape != (M, w.C) or y.shape != (M, w.N):
+        raise ValueError(f"x {x.dtype} {tuple(x.shape)} and y {y.dtype} {tuple(y.shape)} for matrices [{w.N}, {w.C}]")
+    if expert is not None and (expert.dtype != torch.int32 or expert.shape != (M,)):
+        raise ValueError("expert is int32 [M]")
+    with _on_device_of(w.codes):
+        _check(lib().moe_w4_matvec(w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y), _stream(stream)), "moe_w4_matvec")
+
+
+def moe_w4_pack(weights, out: W4, stream=None) -> None:
+    """bf16 or fp32 weights [experts, N, C] into out's 4-bit codes and scales."""
+    _w4_shape(out, weights)
+    dtype = _dtype_code(weights)
+    with _on_device_of(out.codes):
+        _check(lib().moe_w4_pack(dtype, out.experts, out.N, out.C, out.group, _ptr(weights), out.ref, _stream(stream)), "moe_w4_pack")
+
+
+def moe_w4_unpack(w: W4, out, stream=None) -> None:
+    """The weights that w's codes stand for, into out [experts, N, C] (bf16 or fp32)."""
+    _w4_shape(w, out)
+    dtype = _dtype_code(out)
+    with _on_device_of(w.codes):
+        _check(lib().moe_w4_unpack(dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out), _stream(stream)), "moe_w4_unpack")
+
+
 class Plan:
     """Owns a moe_plan_t and the torch-allocated workspace it points into."""
 
@@ -231,6 +311,18 @@ class Plan:
     def moe_layer(self, x, wr, bias, wg, wu, wd, y, stream=None):
         _check(lib().moe_layer(self.handle, _ptr(x), _ptr(wr), _ptr(bias), _ptr(wg), _ptr(wu), _ptr(wd), _ptr(y),
                                _stream(stream)), "moe_layer")
+
+    def moe_layer_few(self, x, wr, bias, wg, wu, wd, y, stream=None):
+        _check(lib().moe_layer_few(self.handle, _ptr(x), _ptr(wr), _ptr(bias), _ptr(wg), _ptr(wu), _ptr(wd), _ptr(y),
+                                   _stream(stream)), "moe_layer_few")
+
+    def moe_layer_few_w4(self, x, wr, bias, wg: W4, wu: W4, wd: W4, y, stream=None):
+        c = self.cfg
+        if not (wg.experts == wu.experts == wd.experts == c.E and wg.group == wu.group == wd.group
+                and (wg.N, wg.C) == (wu.N, wu.C) == (wd.C, wd.N) == (c.F, c.H)):
+            raise ValueError("wg, wu: [E, F, H], wd: [E, H, F], one group size")
+        _check(lib().moe_layer_few_w4(self.handle, _ptr(x), _ptr(wr), _ptr(bias), wg.group, wg.ref, wu.ref, wd.ref, _ptr(y),
+                                      _stream(stream)), "moe_layer_few_w4")
 
     def moe_layer_host(self, h_x, wr, bias, wg, wu, wd, h_y, stream=None):
         """h_x, h_y: HOST tensors (pinned for asynchronous copies); weights: device tensors."""

@@ -136,6 +136,10 @@ size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, s
   const size_t slabs = direct ? (size_t)t.route_slices : 1;
   t.route_logits = filter || (chains && experts > 64) ? (float*)take(sizeof(float) * slabs * (size_t)(c.T > 0 ? c.T : 1) * 256) : nullptr;
   t.route_wnorm2 = filter ? (float*)take(sizeof(float) * 256) : nullptr;
+  if (!c.identity_experts && c.T > 0 && c.T <= MOE_FEW_MAX_TOKENS) {
+    t.few_logits = (float*)take(sizeof(float) * 256 * (size_t)c.T);
+    t.few_sync = (unsigned*)take(sizeof(unsigned) * 4);
+  }
   t.topk_idx = (int*)take(sizeof(int) * (size_t)c.T * c.K);
   t.topk_w = (float*)take(sizeof(float) * (size_t)c.T * c.K);
   t.recv = take(pool_rows * c.H * g.eb);
@@ -219,7 +223,8 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
       cudaMemset(p->s.hist, 0, sizeof(int) * (size_t)g.eff.E) != cudaSuccess ||
       cudaMemset(p->s.ord_exit, 0, sizeof(int) * 2) != cudaSuccess ||
       cudaMemset(p->s.gemm1_done, 0, sizeof(int) * (size_t)(g.P + 4)) != cudaSuccess ||
-      cudaMemset(p->s.clock_probe, 0, 2 * sizeof(unsigned long long)) != cudaSuccess) {
+      cudaMemset(p->s.clock_probe, 0, 2 * sizeof(unsigned long long)) != cudaSuccess ||
+      (p->s.few_sync && cudaMemset(p->s.few_sync, 0, sizeof(unsigned) * 4) != cudaSuccess)) {
     delete p;
     return MOE_ERR_CUDA;
   }

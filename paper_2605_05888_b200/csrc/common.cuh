@@ -19,7 +19,8 @@ __device__ __forceinline__ void set_status(int* status, int code, int detail) {
 
 // Wait sites reported in the detail word of MOE_ERR_TIMEOUT.
 enum WaitSite { kWaitTileTable = 1, kWaitMbarTma = 3, kWaitMbarMma = 4,
-                kWaitMbarEpi = 5, kWaitMbarTmemFree = 6, kWaitTileReady = 7, kWaitItem = 8 };
+                kWaitMbarEpi = 5, kWaitMbarTmemFree = 6, kWaitTileReady = 7, kWaitItem = 8,
+                kWaitGrid = 9 };
 
 struct Scratch {          // device pointers carved out of the caller's workspace
   int* status;            // [4]
@@ -44,6 +45,8 @@ struct Scratch {          // device pointers carved out of the caller's workspac
   unsigned char* group_large;  // [P*8] with recv_planes: which groups of 16 rows hold large numbers
   float* route_logits;    // [T, 256] router logits, more than 64 experts: the chain kernel's, or the tensor-core filter's approximate ones
   int route_slices;       // the slices of h that they are in (route_direct_kernel's: [route_slices, T, 256]); 0: another router
+  float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens; else nullptr)
+  unsigned* few_sync;     // [4]   and its two grid barriers (left as they were found by every launch)
   float* route_wnorm2;    // [256]    squared norms of the router's weight rows, recomputed by every call (filter)
   // moe_layer's internal buffers
   int* topk_idx;

@@ -1,0 +1,359 @@
+// The whole MoE layer (paper Section II-A, steps 1-5) for a few tokens in one launch, on bf16, fp32 or 4-bit expert weights
+// (moe_layer_few, moe_layer_few_w4 of include/moehub.h).
+//
+// As many CTAs as SMs, all resident (a cooperative launch), go through three parts with two grid-wide barriers between them:
+//   router   every CTA forms the logits of a few experts, or of slices of them where there are few experts
+//   gate/up  every CTA selects the picks for itself from the logits, and computes its share of the rows
+//            S[u, t, f] = silu(x_t Wg[e_u, f]) * (x_t Wu[e_u, f]) of the used experts e_0 < e_1 < ...
+//   down     every CTA computes its share of the outputs y[t, h] = sum_u w[u, t] sum_f S[u, t, f] Wd[e_u, h, f]: all the used
+//            experts' columns of a row are in one CTA, so there is no separate combine step
+// No row is copied, and no table is built that only a later launch would read.
+#include "route_common.cuh"
+#include "tc_common.cuh"
+#include "w4_common.cuh"
+
+namespace moehub {
+
+constexpr int kLfThreads = 256;
+constexpr int kLfWarps = kLfThreads / 32;
+constexpr int kLfTokens = MOE_FEW_MAX_TOKENS;
+constexpr int kLfPicks = 32;  // most picks per token
+static_assert(kMaxExperts == kLfThreads, "a thread per expert");
+
+struct LfMatrix {
+  const void* w;                // [E, N, C] of the weights' type, or the codes
+  const __nv_bfloat16* scales;  // [E, C / group, N] (4 bits)
+};
+
+struct LayerFewParams {
+  const void* x;
+  const void* wr;
+  const float* bias;
+  LfMatrix wg, wu, wd;
+  void* y;
+  int T, H, E, K, F, renorm, group, tp;
+  int slices, slice_cols;  // of the router's sums
+  float* logits;           // [slices, T, E]
+  void* inter;             // [used experts, T, F]
+  unsigned* sync;          // two barriers: {arrived, generation} each
+  int* topk_idx;           // the picks and rows per expert, as moe_layer leaves them (every TP shard listed)
+  float* topk_w;
+  int* expert_count;
+  int* status;
+  unsigned long long wait_ns;
+};
+
+// Every CTA of the grid arrives exactly once per launch and barrier, also one whose wait ran out before, so the counters are
+// left as they were found whatever happens.  Everything written before is visible behind it (to loads that miss L1).
+__device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which) {
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    unsigned* arrived = p.sync + 2 * which;
+    int* generation = reinterpret_cast<int*>(p.sync + 2 * which + 1);
+    const int before = ld_acquire(generation);
+    __threadfence();
+    if (atomicAdd(arrived, 1u) == gridDim.x - 1) {
+      atomicExch(arrived, 0u);
+      __threadfence();
+      st_release(generation, before + 1);
+    } else {
+      const unsigned long long t0 = globaltimer();
+      while (ld_acquire(generation) == before) {
+        if (globaltimer() - t0 > p.wait_ns) {
+          set_status(p.status, MOE_ERR_TIMEOUT, kWaitGrid);
+          break;
+        }
+      }
+    }
+    __threadfence();
+  }
+  __syncthreads();
+}
+
+struct LfShared {
+  float red[kLfWarps][kLfTokens];
+  int idx[kLfTokens * kLfPicks];
+  float w[kLfTokens * kLfPicks];
+  unsigned mask[kMaxExperts];           // the tokens that picked an expert
+  int used[kMaxExperts];                // the used experts, ascending
+  int pos[kMaxExperts];                 // and an expert's place among them
+  int warp_used[kLfWarps];
+  float weight[kMaxExperts][kLfTokens]; // of a token for a used expert
+  float logits[kLfTokens * kMaxExperts];
+};
+
+// The logits (or a slice's part of them): a CTA per expert and slice, columns over its threads.
+template <typename T>
+__device__ __forceinline__ void lf_router(const LayerFewParams& p, LfShared& s) {
+  constexpr int N = Vec16<T>::N;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int task = blockIdx.x; task < p.E * p.slices; task += gridDim.x) {
+    const int e = task / p.slices, slice = task % p.slices;
+    const int c0 = slice * p.slice_cols, c1 = min(p.H, c0 + p.slice_cols);
+    float acc[kLfTokens] = {};
+    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += kLfThreads * N) {
+      float w[N];
+      Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)e * p.H + c), w);
+#pragma unroll
+      for (int t = 0; t < kLfTokens; ++t) {
+        if (t >= p.T) break;
+        float v[N], part = 0.0f;
+        Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.x + (size_t)t * p.H + c), v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) part = __fmaf_rn(v[j], w[j], part);
+        acc[t] += part;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kLfTokens; ++t) {
+      if (t >= p.T) break;
+      const float sum = group_sum<32>(acc[t]);
+      if (lane == 0) s.red[warp][t] = sum;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < p.T) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kLfWarps; ++i) sum += s.red[i][threadIdx.x];
+      __stcg(p.logits + ((size_t)slice * p.T + threadIdx.x) * p.E + e, sum);
+    }
+    __syncthreads();
+  }
+}
+
+// Every CTA selects for itself; returns the number of used experts.
+__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s) {
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  for (int i = tid; i < p.T * p.E; i += kLfThreads) {
+    float l = p.bias != nullptr ? p.bias[i % p.E] : 0.0f;
+    float sum = 0.0f;
+    for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
+    s.logits[i] = sum + l;
+  }
+  s.mask[tid] = 0;
+  __syncthreads();
+  if (p.E <= 64) select_topk<32, 2>(s.logits, p.E, p.T, 0, p.E, p.K, p.renorm, s.idx, s.w, nullptr, 1);
+  else select_topk<32, 8>(s.logits, p.E, p.T, 0, p.E, p.K, p.renorm, s.idx, s.w, nullptr, 1);
+  __syncthreads();
+  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
+    atomicOr(&s.mask[s.idx[a]], 1u << (a / p.K));
+    if (blockIdx.x == 0)
+      for (int sh = 0; sh < p.tp; ++sh) {
+        p.topk_idx[a * p.tp + sh] = s.idx[a] * p.tp + sh;
+        p.topk_w[a * p.tp + sh] = s.w[a];
+      }
+  }
+  __syncthreads();
+  const bool mine = s.mask[tid] != 0;
+  if (blockIdx.x == 0)
+    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(s.mask[e / p.tp]);
+  const unsigned b = __ballot_sync(0xffffffffu, mine);
+  if (lane == 0) s.warp_used[warp] = __popc(b);
+  __syncthreads();
+  int before = 0, n = 0;
+#pragma unroll
+  for (int i = 0; i < kLfWarps; ++i) {
+    if (i < warp) before += s.warp_used[i];
+    n += s.warp_used[i];
+  }
+  s.pos[tid] = before + __popc(b & ((1u << lane) - 1u));
+  if (mine) s.used[s.pos[tid]] = tid;
+  __syncthreads();
+  for (int a = tid; a < p.T * p.K; a += kLfThreads) s.weight[s.pos[s.idx[a]]][a / p.K] = s.w[a];
+  __syncthreads();
+  return n;
+}
+
+// The weights' formats: a lane takes VEC consecutive columns.
+template <typename W> struct LfFormat {
+  typedef W X;  // of the rows
+  static constexpr int VEC = Vec16<W>::N;
+  __device__ static __forceinline__ void load(const LfMatrix& m, int e, int N, int C, int, int n, int c, float (&v)[VEC]) {
+    Vec16<W>::unpack(__ldcs(reinterpret_cast<const uint4*>((const W*)m.w + ((size_t)e * N + n) * C + c)), v);
+  }
+};
+struct W4 {};
+template <> struct LfFormat<W4> {
+  typedef __nv_bfloat16 X;
+  static constexpr int VEC = 8;
+  __device__ static __forceinline__ void load(const LfMatrix& m, int e, int N, int C, int group, int n, int c, float (&v)[VEC]) {
+    const uint32_t word = __ldcs((const uint32_t*)m.w + (((size_t)e * N + n) * C + c) / 8);
+    const float scale = __bfloat162float(m.scales[((size_t)e * (C / group) + c / group) * N + n]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = scale * w4_value(word, j);
+  }
+};
+
+// What row n of a matrix gives for the tokens of `mask`: every lane's part of the sums.
+template <typename W>
+__device__ __forceinline__ void lf_dots(const LfMatrix& m, int e, int N, int C, int group, int n, const void* x, unsigned mask, float (&acc)[kLfTokens]) {
+  typedef LfFormat<W> Fmt;
+  typedef typename Fmt::X X;
+  constexpr int PER = Vec16<X>::N;
+  for (int c = threadIdx.x % 32 * Fmt::VEC; c < C; c += 32 * Fmt::VEC) {
+    float w[Fmt::VEC];
+    Fmt::load(m, e, N, C, group, n, c, w);
+#pragma unroll
+    for (int t = 0; t < kLfTokens; ++t) {
+      if (!((mask >> t) & 1u)) continue;
+      float part = 0.0f;
+#pragma unroll
+      for (int q = 0; q < Fmt::VEC / PER; ++q) {
+        float v[PER];
+        Vec16<X>::unpack(__ldcg(reinterpret_cast<const uint4*>((const X*)x + (size_t)t * C + c) + q), v);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) part = __fmaf_rn(v[j], w[q * PER + j], part);
+      }
+      acc[t] += part;
+    }
+  }
+}
+
+__device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
+
+template <typename W>
+__global__ void __launch_bounds__(kLfThreads, 1)
+layer_few_kernel(const __grid_constant__ LayerFewParams p) {
+  typedef typename LfFormat<W>::X X;
+  __shared__ LfShared s;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
+  lf_router<X>(p, s);
+  grid_barrier(p, 0);
+  const int used = lf_select(p, s);
+  const long long rows = (long long)used * p.F;
+  for (long long r = blockIdx.x * kLfWarps + warp; r < rows; r += gridDim.x * kLfWarps) {
+    const int u = (int)(r / p.F), f = (int)(r % p.F), e = s.used[u];
+    const unsigned mask = s.mask[e];
+    float g[kLfTokens] = {}, v[kLfTokens] = {};
+    lf_dots<W>(p.wg, e, p.F, p.H, p.group, f, p.x, mask, g);
+    lf_dots<W>(p.wu, e, p.F, p.H, p.group, f, p.x, mask, v);
+#pragma unroll
+    for (int t = 0; t < kLfTokens; ++t) {
+      if (!((mask >> t) & 1u)) continue;
+      const float a = group_sum<32>(g[t]), b = group_sum<32>(v[t]);
+      if (lane == 0) ((X*)p.inter)[((size_t)u * p.T + t) * p.F + f] = from_float<X>(lf_silu_mul(a, b));
+    }
+  }
+  grid_barrier(p, 1);
+  for (int h = blockIdx.x * kLfWarps + warp; h < p.H; h += gridDim.x * kLfWarps) {
+    float total[kLfTokens] = {};
+    for (int u = 0; u < used; ++u) {
+      const unsigned mask = s.mask[s.used[u]];
+      float acc[kLfTokens] = {};
+      lf_dots<W>(p.wd, s.used[u], p.H, p.F, p.group, h, (const X*)p.inter + (size_t)u * p.T * p.F, mask, acc);
+#pragma unroll
+      for (int t = 0; t < kLfTokens; ++t)
+        if ((mask >> t) & 1u) total[t] = __fmaf_rn(s.weight[u][t], acc[t], total[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < kLfTokens; ++t) {
+      if (t >= p.T) break;
+      const float sum = group_sum<32>(total[t]);
+      if (lane == 0) ((X*)p.y)[(size_t)t * p.H + h] = from_float<X>(sum);
+    }
+  }
+}
+
+static cudaError_t launch_cooperative(void (*kern)(LayerFewParams), int grid, size_t smem, cudaStream_t st, const LayerFewParams& q) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kLfThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, q);
+}
+
+// The checks and the launch that both entry points share.
+static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bias, LfMatrix wg, LfMatrix wu, LfMatrix wd, int group,
+                     void* y, cudaStream_t st) {
+  const moe_config_t& c = p->cfg;
+  p->launches = 0;
+  if (c.T == 0) return MOE_OK;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) return MOE_ERR_CUDA;
+  if (device != p->device) return MOE_ERR_ARG;
+  LayerFewParams q = {};
+  q.x = x;
+  q.wr = wr;
+  q.bias = bias;
+  q.wg = wg;
+  q.wu = wu;
+  q.wd = wd;
+  q.y = y;
+  q.T = c.T;
+  q.H = c.H;
+  q.E = p->route_E;  // (an expert's TP shards lie next to one another in its matrices: here it is computed whole)
+  q.K = p->route_K;
+  q.F = c.F * p->tp;
+  q.renorm = c.renormalize;
+  q.group = group;
+  q.tp = p->tp;
+  // about a task per CTA, no slice under 256 columns; the scratch holds 256 sums per token
+  q.slices = max(1, min(min(p->sm_count, 256) / q.E, min(16, c.H / 256)));
+  const int unit = 8;
+  q.slice_cols = ((c.H + q.slices - 1) / q.slices + unit - 1) / unit * unit;
+  q.slices = (c.H + q.slice_cols - 1) / q.slice_cols;
+  q.logits = p->s.few_logits;
+  q.inter = p->s.inter;
+  q.sync = p->s.few_sync;
+  q.topk_idx = p->s.topk_idx;
+  q.topk_w = p->s.topk_w;
+  q.expert_count = p->s.expert_count;
+  q.status = p->s.status;
+  q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
+  auto kern = group > 0 ? layer_few_kernel<W4> : c.dtype == MOE_DTYPE_BF16 ? layer_few_kernel<__nv_bfloat16> : layer_few_kernel<float>;
+  cudaError_t e = launch_cooperative(kern, p->sm_count, 0, st, q);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    p->cuda_error = (int)e;
+    p->cuda_error_step = 3;
+    return MOE_ERR_CUDA;
+  }
+  p->launches = 1;
+  return MOE_OK;
+}
+
+static int check_layer_few(const moe_plan* p, const void* x, const void* wr, const void* y) {
+  if (!p || !wr) return MOE_ERR_ARG;
+  if (p->cfg.T > 0 && (!x || !y)) return MOE_ERR_ARG;
+  if (p->cfg.identity_experts) return MOE_ERR_ARG;
+  if (p->cfg.T > MOE_FEW_MAX_TOKENS) return MOE_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(wr) | reinterpret_cast<uintptr_t>(y)) & 15) return MOE_ERR_ALIGN;
+  return MOE_OK;
+}
+
+}  // namespace moehub
+
+using namespace moehub;
+
+extern "C" {
+
+int moe_layer_few(moe_plan_t* p, const void* d_x, const void* d_wr, const float* d_bias, const void* d_wg, const void* d_wu,
+                  const void* d_wd, void* d_y, void* stream) {
+  int rc = check_layer_few(p, d_x, d_wr, d_y);
+  if (rc != MOE_OK) return rc;
+  if (!d_wg || !d_wu || !d_wd) return MOE_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(d_wg) | reinterpret_cast<uintptr_t>(d_wu) | reinterpret_cast<uintptr_t>(d_wd)) & 15) return MOE_ERR_ALIGN;
+  return layer_few(p, d_x, d_wr, d_bias, {d_wg, nullptr}, {d_wu, nullptr}, {d_wd, nullptr}, 0, d_y, (cudaStream_t)stream);
+}
+
+int moe_layer_few_w4(moe_plan_t* p, const void* d_x, const void* d_wr, const float* d_bias, int32_t group, const moe_w4_t* wg,
+                     const moe_w4_t* wu, const moe_w4_t* wd, void* d_y, void* stream) {
+  int rc = check_layer_few(p, d_x, d_wr, d_y);
+  if (rc != MOE_OK) return rc;
+  if (p->cfg.dtype != MOE_DTYPE_BF16) return MOE_ERR_UNSUPPORTED;
+  const int F = p->cfg.F * p->tp;
+  if ((rc = w4_check(wg, p->route_E, F, p->cfg.H, group)) != MOE_OK) return rc;
+  if ((rc = w4_check(wu, p->route_E, F, p->cfg.H, group)) != MOE_OK) return rc;
+  if ((rc = w4_check(wd, p->route_E, p->cfg.H, F, group)) != MOE_OK) return rc;
+  auto matrix = [](const moe_w4_t* w) { return LfMatrix{w->codes, (const __nv_bfloat16*)w->scales}; };
+  return layer_few(p, d_x, d_wr, d_bias, matrix(wg), matrix(wu), matrix(wd), group, d_y, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,352 @@
+"""The MoE layer for a few tokens in one launch, on bf16, fp32 and 4-bit experts, against its definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import w4_helpers as R
+from paper_2605_05888_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+class Layer:
+    """Random inputs of a layer and what the calls need.  group 0: plain weights."""
+
+    def __init__(self, T, H, E, K, F, dtype=BF16, group=0, renorm=0, bias=False, seed=1, std=0.05, router_std=0.05, **cfg):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.T, self.H, self.E, self.K, self.F, self.dtype, self.group, self.renorm = T, H, E, K, F, dtype, group, renorm
+
+        def normal(std, *shape):
+            return torch.empty(shape, dtype=dtype, device="cuda").normal_(0.0, std, generator=g)
+        self.x, self.wr = normal(1.0, T, H), normal(router_std, E, H)
+        self.bias = torch.empty(E, device="cuda").normal_(0.0, 0.5, generator=g) if bias else None
+        shapes = ((E, F, H), (E, F, H), (E, H, F))
+        if group:
+            self.w = [B.W4(*R.random_w4(g, std, *s, group=group)) for s in shapes]
+        else:
+            self.w = [normal(std, *s) for s in shapes]
+        self.plan = B.Plan(B.make_config(T, H, E, 1, K, F, B.DTYPE_FP32 if dtype == FP32 else B.DTYPE_BF16, renormalize=renorm, **cfg))
+        self.room = torch.full((T * H + 64,), 55.0, dtype=dtype, device="cuda")
+        self.y = self.room[:T * H].view(T, H)
+
+    def call(self, x=None, y=None, plan=None, stream=None):
+        plan, x, y = plan or self.plan, self.x if x is None else x, self.y if y is None else y
+        (plan.moe_layer_few_w4 if self.group else plan.moe_layer_few)(x, self.wr, self.bias, *self.w, y, stream=stream)
+        return y
+
+    def matrix(self, i):
+        w = self.w[i]
+        return (lambda e: R.weights(w.codes[e], w.scales[e])) if self.group else (lambda e: w[e].double())
+
+    def check(self):
+        self.y.fill_(77.0)
+        self.call()
+        assert self.plan.moe_last_launch_count() == 1
+        assert self.plan.moe_last_status() == (0, 0)
+        idx = self.plan.layer_tensor(0).long()
+        logits, dl, w, y, bound = R.layer(self.x.double(), self.wr.double(), self.bias, self.matrix(0), self.matrix(1), self.matrix(2), self.K,
+                                          self.renorm, idx, self.dtype)
+        R.check_picks(idx, logits, dl)
+        R.assert_within(self.y, y, bound, "y")
+        assert (self.room[self.T * self.H:] == 55.0).all()
+        assert np.allclose(self.plan.layer_tensor(1).double().cpu().numpy(), w.cpu().numpy(), rtol=1e-3)
+        assert torch.equal(self.plan.layer_tensor(3).long().cpu(), torch.bincount(idx.flatten().cpu(), minlength=self.E))
+        return self.y
+
+
+# T, H, E, K, F: one token and sixteen, one expert, as many picks as experts, one used expert and all, H and F that end inside a
+# lane's vectors and a block of columns, more and fewer rows than the GPU has warps
+BF16_SHAPES = [(1, 8, 1, 1, 8), (1, 2048, 60, 4, 1408), (2, 136, 3, 3, 72), (3, 264, 5, 2, 1000), (4, 1024, 8, 2, 520), (5, 512, 2, 1, 64), (7, 8, 4, 2, 4104),
+               (8, 4104, 16, 2, 8), (8, 256, 256, 8, 128), (9, 640, 7, 7, 328), (13, 1000, 33, 5, 248), (16, 768, 64, 6, 1032), (16, 128, 256, 32, 64),
+               (16, 7168, 4, 1, 512), (11, 96, 130, 3, 2056)]
+FP32_SHAPES = [(1, 4, 1, 1, 4), (1, 1024, 16, 2, 2048), (3, 1020, 16, 2, 2044), (2, 132, 3, 3, 36), (8, 100, 9, 4, 516), (9, 512, 256, 8, 60), (16, 260, 5, 5, 260),
+               (16, 68, 64, 16, 12), (6, 2052, 2, 1, 4)]
+W4_SHAPES = [(1, 1, 1, 1, 1), (1, 16, 60, 4, 11), (2, 2, 3, 3, 1), (4, 5, 8, 2, 7), (8, 1, 4, 2, 33), (8, 33, 16, 2, 1), (9, 3, 7, 7, 3), (13, 7, 33, 5, 2),
+             (16, 6, 64, 6, 9), (16, 2, 256, 32, 1), (16, 56, 4, 1, 4), (5, 4, 2, 1, 4)]
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("shape", BF16_SHAPES, ids=str)
+def test_layer_bf16(shape, renorm):
+    Layer(*shape, renorm=renorm, bias=bool(renorm)).check()
+
+
+@pytest.mark.parametrize("renorm", [0, 1])
+@pytest.mark.parametrize("shape", FP32_SHAPES, ids=str)
+def test_layer_fp32(shape, renorm):
+    Layer(*shape, dtype=FP32, renorm=renorm, bias=bool(renorm)).check()
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("shape", W4_SHAPES, ids=str)
+def test_layer_w4(shape, group):
+    T, h, E, K, f = shape
+    Layer(T, h * group, E, K, f * group, group=group, renorm=group == 64, bias=group == 32).check()
+
+
+@pytest.mark.parametrize("T", range(1, 17))
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "w4"])
+def test_every_token_count(T, kind):
+    Layer(T, 384, 12, 3, 320, dtype=FP32 if kind == "fp32" else BF16, group=64 if kind == "w4" else 0, seed=T).check()
+
+
+def kinds(f):
+    return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
+
+
+@kinds
+def test_all_tokens_on_one_expert(dtype, group):
+    s = Layer(16, 512, 8, 1, 256, dtype=dtype, group=group)
+    s.bias = torch.full((8,), float("-inf"), device="cuda")
+    s.bias[5] = 0.0
+    s.check()
+    assert (s.plan.layer_tensor(0) == 5).all()
+
+
+def test_equal_experts_lowest_index_first():
+    s = Layer(6, 1000, 40, 5, 64)
+    s.wr[1:] = s.wr[:1]
+    s.check()
+    assert (s.plan.layer_tensor(0).cpu() == torch.arange(5, dtype=torch.int32)).all()
+
+
+def test_router_biases_of_the_lowest_values():
+    """Experts masked by -inf or by the lowest fp32 number are picked last, in ascending order, with no weight."""
+    for low in (float("-inf"), torch.finfo(FP32).min):
+        s = Layer(3, 256, 6, 4, 64, bias=True)
+        s.bias[[0, 2, 3, 5]] = low
+        s.call()
+        idx, w = s.plan.layer_tensor(0).cpu(), s.plan.layer_tensor(1).cpu()
+        assert all(sorted(r[:2].tolist()) == [1, 4] and r[2:].tolist() == [0, 2] for r in idx)
+        assert (w[:, 2:] == 0).all() and np.allclose(w.sum(1).numpy(), 1.0, atol=1e-6)
+        assert s.y.isfinite().all()
+
+
+@kinds
+def test_nan_and_infinity_stay_with_their_token(dtype, group):
+    """A token that holds a NaN or an infinity, and an expert with a weight that is not finite, leave the other tokens alone."""
+    s = Layer(12, 512, 16, 2, 256, dtype=dtype, group=group, seed=8)
+    want = s.call().clone()
+    x = s.x.clone()
+    x[3, 100] = float("nan")
+    x[7, 511] = float("inf")
+    y = torch.zeros_like(want)
+    s.call(x=x, y=y)
+    rest = [t for t in range(12) if t not in (3, 7)]
+    assert torch.equal(y[rest], want[rest]) and y[3].isnan().all() and not y[7].isfinite().all()
+    s.call()
+    idx = s.plan.layer_tensor(0).cpu()
+    e = int(idx[0, 0])
+    for i, name in enumerate(("gate", "up", "down")):
+        w = s.w[i]
+        t = w.scales if group else w
+        keep = t[e].clone()
+        t[e] = float("inf")
+        s.call(y=y)
+        for tok in range(12):
+            if e in idx[tok].tolist():
+                assert not y[tok].isfinite().all(), (name, tok)
+            else:
+                assert torch.equal(y[tok], want[tok]), (name, tok)
+        t[e] = keep
+
+
+@kinds
+def test_same_bytes_every_time(dtype, group):
+    s = Layer(10, 1024, 24, 3, 768, dtype=dtype, group=group)
+    first = s.call().clone()
+    for _ in range(5):
+        s.y.zero_()
+        assert torch.equal(s.call(), first)
+
+
+@kinds
+def test_tensor_parallel_shards_change_nothing(dtype, group):
+    s = Layer(5, 512, 8, 2, 512, dtype=dtype, group=group, renorm=1)
+    first = s.call().clone()
+    tp = B.Plan(B.make_config(5, 512, 8, 1, 2, 512, s.plan.cfg.dtype, renormalize=1, tp_shards=4))
+    assert torch.equal(s.call(plan=tp, y=torch.empty_like(first)), first)
+    idx, w = s.plan.layer_tensor(0), s.plan.layer_tensor(1)
+    shards = (idx[..., None] * 4 + torch.arange(4, device="cuda", dtype=torch.int32)).flatten(1)
+    assert torch.equal(tp.layer_tensor(0), shards) and torch.equal(tp.layer_tensor(1), w.repeat_interleave(4, 1))
+    assert torch.equal(tp.layer_tensor(3), s.plan.layer_tensor(3).repeat_interleave(4))
+
+
+@pytest.mark.parametrize("mode", range(4))
+def test_between_calls_of_the_layer(mode):
+    """moe_layer and moe_layer_few take turns on one plan: neither disturbs the other, in any dispatch scheme."""
+    s = Layer(12, 512, 16, 2, 256, dispatch_mode=mode)
+    want, few = torch.empty_like(s.y), s.call().clone()
+    s.plan.moe_layer(s.x, s.wr, s.bias, *s.w, want)
+    y = torch.empty_like(s.y)
+    for _ in range(3):
+        assert torch.equal(s.call(), few)
+        s.plan.moe_layer(s.x, s.wr, s.bias, *s.w, y)
+        assert torch.equal(y, want) and s.plan.moe_last_status() == (0, 0)
+
+
+@kinds
+def test_captured_and_replayed(dtype, group):
+    s = Layer(6, 768, 12, 3, 512, dtype=dtype, group=group)
+    want = s.call().clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.call()
+        s.call()
+    x2 = s.x.flip(0).clone()
+    for x, y in ((s.x.clone(), want), (x2, want.flip(0))):
+        s.x.copy_(x)
+        s.y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.y, y)
+    s.y.zero_()
+    assert torch.equal(s.call(), want.flip(0))
+
+
+@kinds
+def test_two_plans_on_two_streams_at_once(dtype, group):
+    """Two calls whose CTAs each wait for one another: a cooperative launch starts whole or not at all."""
+    a, b = Layer(4, 2048, 16, 2, 1024, dtype=dtype, group=group, seed=1), Layer(9, 1024, 16, 4, 2048, dtype=dtype, group=group, seed=2)
+    wa, wb = a.call().clone(), b.call().clone()
+    torch.cuda.synchronize()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    a.y.zero_(), b.y.zero_()
+    torch.cuda.synchronize()
+    for _ in range(50):
+        a.call(stream=sa)
+        b.call(stream=sb)
+    torch.cuda.synchronize()
+    assert a.plan.moe_last_status() == (0, 0) and b.plan.moe_last_status() == (0, 0)
+    assert torch.equal(a.y, wa) and torch.equal(b.y, wb)
+
+
+@kinds
+def test_beside_a_kernel_that_fills_the_gpu(dtype, group):
+    s = Layer(4, 1024, 16, 2, 1024, dtype=dtype, group=group)
+    want = s.call().clone()
+    big = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    other, here = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        for _ in range(20):
+            big @ big
+    for _ in range(20):
+        s.call(stream=here)
+    torch.cuda.synchronize()
+    assert s.plan.moe_last_status() == (0, 0) and torch.equal(s.y, want)
+
+
+def test_wait_that_runs_out_is_reported():
+    """A limit of one nanosecond: the barriers give up, the status says so, and the plan's counters are as before."""
+    s = Layer(2, 512, 8, 2, 256, wait_limit_ns=1)
+    s.call()
+    code, detail = s.plan.moe_last_status()
+    assert B.strerror(code) == "bounded device-side wait ran out" and detail == 9
+    s.call()
+    assert s.plan.moe_last_status()[0] == code
+    Layer(2, 512, 8, 2, 256).check()
+
+
+def test_empty_batch():
+    plan = B.Plan(B.make_config(0, 64, 4, 1, 2, 64, B.DTYPE_BF16))
+    w = torch.zeros(4, 64, 64, dtype=BF16, device="cuda")
+    plan.moe_layer_few(None, torch.zeros(4, 64, dtype=BF16, device="cuda"), None, w, w, w, None)
+    assert plan.moe_last_launch_count() == 0
+
+
+def test_calls_refuse_what_they_cannot_take():
+    s, q = Layer(4, 128, 4, 2, 64), Layer(4, 128, 4, 2, 64, group=64)
+
+    def code(f, *a):
+        with pytest.raises(B.MoeError) as err:
+            f(*a)
+        return err.value.code
+
+    wide = B.Plan(B.make_config(17, 128, 4, 1, 2, 64, B.DTYPE_BF16))
+    x17 = torch.zeros(17, 128, dtype=BF16, device="cuda")
+    assert code(wide.moe_layer_few, x17, s.wr, None, *s.w, x17) == -3
+    assert code(wide.moe_layer_few_w4, x17, s.wr, None, *q.w, x17) == -3
+    ident = B.Plan(B.make_config(4, 128, 4, 1, 2, 0, B.DTYPE_BF16, identity_experts=1))
+    assert code(ident.moe_layer_few, s.x, s.wr, None, *s.w, s.y) == -1
+    fp32 = B.Plan(B.make_config(4, 128, 4, 1, 2, 64, B.DTYPE_FP32))
+    assert code(fp32.moe_layer_few_w4, s.x, s.wr, None, *q.w, s.y) == -3
+    for missing in range(7):
+        args = [s.x, s.wr, None, *s.w, s.y]
+        if missing == 2:
+            continue
+        args[missing] = None
+        assert code(s.plan.moe_layer_few, *args) == -1, missing
+        args = [s.x, s.wr, None, *s.w, s.y]
+        args[missing] = args[missing].data_ptr() + 8
+        assert code(s.plan.moe_layer_few, *args) == -2, missing
+    other = Layer(4, 128, 4, 2, 64, group=32)
+    with pytest.raises(ValueError):
+        s.plan.moe_layer_few_w4(s.x, s.wr, None, q.w[0], other.w[1], q.w[2], s.y)
+    with pytest.raises(ValueError):
+        s.plan.moe_layer_few_w4(s.x, s.wr, None, q.w[0], q.w[1], q.w[0], s.y)
+
+
+def test_weights_beyond_four_gigabytes():
+    E, H, F = 40, 8192, 8192
+    w = [torch.empty(E, F, H, dtype=BF16, device="cuda").normal_(0.0, 0.02) for _ in range(2)]
+    w.append(w[0].view(E, H, F))
+    s = Layer(2, 8, E, 2, 8)
+    s.H, s.F, s.w = H, F, w
+    s.x = torch.randn(2, H, device="cuda", dtype=BF16)
+    s.wr = torch.randn(E, H, device="cuda").mul_(0.02).to(BF16)
+    s.bias = torch.full((E,), float("-inf"), device="cuda")
+    s.bias[[0, 36, 39]] = 0.0                   # more than 2^32 bytes apart
+    s.plan = B.Plan(B.make_config(2, H, E, 1, 2, F, B.DTYPE_BF16))
+    s.room = torch.full((2 * H + 64,), 55.0, dtype=BF16, device="cuda")
+    s.y = s.room[:2 * H].view(2, H)
+    s.check()
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_prefill_and_decoding_on_the_same_4bit_experts(group):
+    """As a user has it: dense experts are packed once; a prompt goes through moe_layer on the unpacked weights, the tokens after it
+    through the one-launch layer on the codes; a shared expert's projection beside it is a product of its own."""
+    H, E, K, F, T = 512, 16, 2, 384, 200
+    g = torch.Generator(device="cuda").manual_seed(9)
+
+    def normal(std, *shape):
+        return torch.empty(shape, dtype=BF16, device="cuda").normal_(0.0, std, generator=g)
+
+    dense = [normal(0.05, E, F, H), normal(0.05, E, F, H), normal(0.05, E, H, F)]
+    wr, x = normal(0.05, E, H), normal(1.0, T, H)
+    packed, back = [], []
+    for w in dense:
+        packed.append(B.W4.empty(w.shape[1], w.shape[2], group, experts=E))
+        B.moe_w4_pack(w, packed[-1])
+        back.append(torch.empty_like(w))
+        B.moe_w4_unpack(packed[-1], back[-1])
+        # the form's own error: half a step of the scale at most, and what the scale's and the weight's rounding to bf16 add
+        step = packed[-1].scales.double().transpose(1, 2).repeat_interleave(group, dim=2)
+        assert ((back[-1].double() - w.double()).abs() <= step * (0.5 + 7 * 2.0 ** -8) + 2.0 ** -8 * w.double().abs()).all()
+    prompt, y = B.Plan(B.make_config(T, H, E, 1, K, F, B.DTYPE_BF16)), torch.empty_like(x)
+    prompt.moe_layer(x, wr, None, *back, y)
+    shared = B.W4(packed[0].codes[3], packed[0].scales[3])
+    for T1 in (1, 5, 16):
+        plan = B.Plan(B.make_config(T1, H, E, 1, K, F, B.DTYPE_BF16))
+        few, proj = torch.empty(T1, H, dtype=BF16, device="cuda"), torch.empty(T1, F, dtype=BF16, device="cuda")
+        for t0 in range(0, 48, T1):
+            rows = x[t0:t0 + T1]
+            if rows.shape[0] < T1:
+                break
+            plan.moe_layer_few_w4(rows, wr, None, *packed, few)
+            B.moe_w4_matvec(shared, rows, None, proj)
+            # the definition on the unrounded 4-bit weights
+            idx = plan.layer_tensor(0).long()
+            m = [lambda e, w=w: R.weights(w.codes[e], w.scales[e]) for w in packed]
+            logits, dl, _, want, bound = R.layer(rows.double(), wr.double(), None, *m, K, 0, idx, BF16)
+            R.check_picks(idx, logits, dl)
+            R.assert_within(few, want, bound, "decoded tokens")
+            p, pb = R.matvec(R.weights(shared.codes, shared.scales), rows.double())
+            R.assert_within(proj, p, pb + R.HALF[BF16] * (p.abs() + pb), "projection")
+            # and the prompt's rows are the same tokens on weights rounded to bf16
+            assert torch.equal(idx, prompt.layer_tensor(0)[t0:t0 + T1].long())
+            diff = (few.double() - y[t0:t0 + T1].double()).norm() / y[t0:t0 + T1].double().norm()
+            assert diff < 2e-2  # (three roundings of the weights and two of what is stored, each 2^-8 of a value at most)
