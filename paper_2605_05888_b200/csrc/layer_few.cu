@@ -9,13 +9,12 @@
 //            experts' columns of a row are in one CTA, so there is no separate combine step
 // No row is copied, and no table is built that only a later launch would read.
 #include "route_common.cuh"
-#include "tc_common.cuh"
-#include "w4_common.cuh"
+#include "row_stream.cuh"
 
 namespace moehub {
 
-constexpr int kLfThreads = 256;
-constexpr int kLfWarps = kLfThreads / 32;
+constexpr int kLfThreads = kRsThreads;
+constexpr int kLfWarps = kRsWarps;
 constexpr int kLfTokens = MOE_FEW_MAX_TOKENS;
 constexpr int kLfPicks = 32;  // most picks per token
 static_assert(kMaxExperts == kLfThreads, "a thread per expert");
@@ -71,20 +70,23 @@ __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which)
 }
 
 struct LfShared {
+  float w[kLfTokens * kLfPicks];               // the picks' weights
+  int used[kMaxExperts];                       // the used experts, ascending
+  unsigned short mask[kMaxExperts];            // the tokens that picked each
+  unsigned char pick[kMaxExperts][kLfTokens];  // which of its picks the expert is for a token
+  int warp_used[kLfWarps];
+};
+struct LfSelect {  // where the rows are streamed through later
   float red[kLfWarps][kLfTokens];
   int idx[kLfTokens * kLfPicks];
-  float w[kLfTokens * kLfPicks];
-  unsigned mask[kMaxExperts];           // the tokens that picked an expert
-  int used[kMaxExperts];                // the used experts, ascending
-  int pos[kMaxExperts];                 // and an expert's place among them
-  int warp_used[kLfWarps];
-  float weight[kMaxExperts][kLfTokens]; // of a token for a used expert
+  unsigned mask[kMaxExperts];
+  int pos[kMaxExperts];  // a used expert's number
   float logits[kLfTokens * kMaxExperts];
 };
 
 // The logits (or a slice's part of them): a CTA per expert and slice, columns over its threads.
 template <typename T>
-__device__ __forceinline__ void lf_router(const LayerFewParams& p, LfShared& s) {
+__device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) {
   constexpr int N = Vec16<T>::N;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   for (int task = blockIdx.x; task < p.E * p.slices; task += gridDim.x) {
@@ -122,31 +124,30 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfShared& s) 
 }
 
 // Every CTA selects for itself; returns the number of used experts.
-__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s) {
+__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   for (int i = tid; i < p.T * p.E; i += kLfThreads) {
-    float l = p.bias != nullptr ? p.bias[i % p.E] : 0.0f;
     float sum = 0.0f;
     for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
-    s.logits[i] = sum + l;
+    q.logits[i] = p.bias != nullptr ? sum + p.bias[i % p.E] : sum;
   }
-  s.mask[tid] = 0;
+  q.mask[tid] = 0;
   __syncthreads();
-  if (p.E <= 64) select_topk<32, 2>(s.logits, p.E, p.T, 0, p.E, p.K, p.renorm, s.idx, s.w, nullptr, 1);
-  else select_topk<32, 8>(s.logits, p.E, p.T, 0, p.E, p.K, p.renorm, s.idx, s.w, nullptr, 1);
+  if (p.E <= 64) select_topk<32, 2>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
+  else select_topk<32, 8>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   __syncthreads();
   for (int a = tid; a < p.T * p.K; a += kLfThreads) {
-    atomicOr(&s.mask[s.idx[a]], 1u << (a / p.K));
+    atomicOr(&q.mask[q.idx[a]], 1u << (a / p.K));
     if (blockIdx.x == 0)
       for (int sh = 0; sh < p.tp; ++sh) {
-        p.topk_idx[a * p.tp + sh] = s.idx[a] * p.tp + sh;
+        p.topk_idx[a * p.tp + sh] = q.idx[a] * p.tp + sh;
         p.topk_w[a * p.tp + sh] = s.w[a];
       }
   }
   __syncthreads();
-  const bool mine = s.mask[tid] != 0;
+  const bool mine = q.mask[tid] != 0;
   if (blockIdx.x == 0)
-    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(s.mask[e / p.tp]);
+    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(q.mask[e / p.tp]);
   const unsigned b = __ballot_sync(0xffffffffu, mine);
   if (lane == 0) s.warp_used[warp] = __popc(b);
   __syncthreads();
@@ -156,110 +157,86 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s) {
     if (i < warp) before += s.warp_used[i];
     n += s.warp_used[i];
   }
-  s.pos[tid] = before + __popc(b & ((1u << lane) - 1u));
-  if (mine) s.used[s.pos[tid]] = tid;
+  const int pos = before + __popc(b & ((1u << lane) - 1u));
+  q.pos[tid] = pos;
+  if (mine) {
+    s.used[pos] = tid;
+    s.mask[pos] = (unsigned short)q.mask[tid];
+  }
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += kLfThreads) s.weight[s.pos[s.idx[a]]][a / p.K] = s.w[a];
+  for (int a = tid; a < p.T * p.K; a += kLfThreads) s.pick[q.pos[q.idx[a]]][a / p.K] = (unsigned char)(a % p.K);
   __syncthreads();
   return n;
 }
 
-// The weights' formats: a lane takes VEC consecutive columns.
-template <typename W> struct LfFormat {
-  typedef W X;  // of the rows
-  static constexpr int VEC = Vec16<W>::N;
-  __device__ static __forceinline__ void load(const LfMatrix& m, int e, int N, int C, int, int n, int c, float (&v)[VEC]) {
-    Vec16<W>::unpack(__ldcs(reinterpret_cast<const uint4*>((const W*)m.w + ((size_t)e * N + n) * C + c)), v);
-  }
-};
-struct W4 {};
-template <> struct LfFormat<W4> {
-  typedef __nv_bfloat16 X;
-  static constexpr int VEC = 8;
-  __device__ static __forceinline__ void load(const LfMatrix& m, int e, int N, int C, int group, int n, int c, float (&v)[VEC]) {
-    const uint32_t word = __ldcs((const uint32_t*)m.w + (((size_t)e * N + n) * C + c) / 8);
-    const float scale = __bfloat162float(m.scales[((size_t)e * (C / group) + c / group) * N + n]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = scale * w4_value(word, j);
-  }
-};
-
-// What row n of a matrix gives for the tokens of `mask`: every lane's part of the sums.
-template <typename W>
-__device__ __forceinline__ void lf_dots(const LfMatrix& m, int e, int N, int C, int group, int n, const void* x, unsigned mask, float (&acc)[kLfTokens]) {
-  typedef LfFormat<W> Fmt;
-  typedef typename Fmt::X X;
-  constexpr int PER = Vec16<X>::N;
-  for (int c = threadIdx.x % 32 * Fmt::VEC; c < C; c += 32 * Fmt::VEC) {
-    float w[Fmt::VEC];
-    Fmt::load(m, e, N, C, group, n, c, w);
-#pragma unroll
-    for (int t = 0; t < kLfTokens; ++t) {
-      if (!((mask >> t) & 1u)) continue;
-      float part = 0.0f;
-#pragma unroll
-      for (int q = 0; q < Fmt::VEC / PER; ++q) {
-        float v[PER];
-        Vec16<X>::unpack(__ldcg(reinterpret_cast<const uint4*>((const X*)x + (size_t)t * C + c) + q), v);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) part = __fmaf_rn(v[j], w[q * PER + j], part);
-      }
-      acc[t] += part;
-    }
-  }
-}
-
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
-template <typename W>
+template <typename W, int NT>
 __global__ void __launch_bounds__(kLfThreads, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
-  typedef typename LfFormat<W>::X X;
+  typedef typename RsFormat<W>::X X;
+  typedef RsSizes<W, NT> Z;
+  extern __shared__ __align__(128) unsigned char dynamic[];
   __shared__ LfShared s;
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  static_assert(sizeof(LfSelect) <= Z::RING, "the selection's tables lie in the ring");
+  LfSelect& q = *reinterpret_cast<LfSelect*>(dynamic);
+  float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
+  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
   if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
-  lf_router<X>(p, s);
+  lf_router<X>(p, q);
   grid_barrier(p, 0);
-  const int used = lf_select(p, s);
-  const long long rows = (long long)used * p.F;
-  for (long long r = blockIdx.x * kLfWarps + warp; r < rows; r += gridDim.x * kLfWarps) {
-    const int u = (int)(r / p.F), f = (int)(r % p.F), e = s.used[u];
-    const unsigned mask = s.mask[e];
-    float g[kLfTokens] = {}, v[kLfTokens] = {};
-    lf_dots<W>(p.wg, e, p.F, p.H, p.group, f, p.x, mask, g);
-    lf_dots<W>(p.wu, e, p.F, p.H, p.group, f, p.x, mask, v);
+  const RsList list{s.used, s.mask, lf_select(p, s, q)};
+
+  // gate and up rows of the used experts
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.group, p.E};
+  typedef RowStream<W, NT, kRsPairs> Up;
+  Up up(gate_up, list, ring);
+  auto finish_up = [&](int u, int row, int n0, int, const float (&sum)[Z::REGS]) {
+    const unsigned mask = s.mask[u];
 #pragma unroll
-    for (int t = 0; t < kLfTokens; ++t) {
-      if (!((mask >> t) & 1u)) continue;
-      const float a = group_sum<32>(g[t]), b = group_sum<32>(v[t]);
-      if (lane == 0) ((X*)p.inter)[((size_t)u * p.T + t) * p.F + f] = from_float<X>(lf_silu_mul(a, b));
+    for (int j = 0; j < Z::REGS; ++j) {
+      const int t = up.token(j), f = up.row_of(j);
+      float v = 0.0f;
+      if (Up::kMma && j % 4 < 2) v = lf_silu_mul(sum[j], sum[Up::kMma ? j + 2 : j]);
+      if (!Up::kMma) v = lf_silu_mul(sum[j], __shfl_down_sync(0xffffffffu, sum[j], kRsRun));
+      if ((Up::kMma ? j % 4 < 2 : threadIdx.x % 32 < kRsRun) && f < n0 && ((mask >> t) & 1u))
+        ((X*)p.inter)[((size_t)u * p.T + t) * p.F + row + f] = from_float<X>(v);
     }
-  }
+  };
+  up.run(nullptr, slots, [](int, int) { return 0.0f; }, finish_up);
+
+  // the outputs; the first down rows are on their way while the other CTAs finish
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, (long long)p.T * p.F, p.H, p.F, p.group, p.E};
+  typedef RowStream<W, NT, kRsSum> Down;
+  Down down(down_op, list, ring);
+  Down start = down;
+  down.prefetch();
+  __syncthreads();
+  up.join(slots, finish_up);
   grid_barrier(p, 1);
-  for (int h = blockIdx.x * kLfWarps + warp; h < p.H; h += gridDim.x * kLfWarps) {
-    float total[kLfTokens] = {};
-    for (int u = 0; u < used; ++u) {
-      const unsigned mask = s.mask[s.used[u]];
-      float acc[kLfTokens] = {};
-      lf_dots<W>(p.wd, s.used[u], p.H, p.F, p.group, h, (const X*)p.inter + (size_t)u * p.T * p.F, mask, acc);
+  auto finish_down = [&](int, int row, int n0, int n1, const float (&sum)[Z::REGS]) {
 #pragma unroll
-      for (int t = 0; t < kLfTokens; ++t)
-        if ((mask >> t) & 1u) total[t] = __fmaf_rn(s.weight[u][t], acc[t], total[t]);
+    for (int j = 0; j < Z::REGS; ++j) {
+      const int t = down.token(j), r = down.row_of(j);
+      const bool second = down.run_of(j) == 1;
+      if (t < p.T && r < (second ? n1 : n0)) ((X*)p.y)[(size_t)t * p.H + row + (second ? n0 : 0) + r] = from_float<X>(sum[j]);
     }
-#pragma unroll
-    for (int t = 0; t < kLfTokens; ++t) {
-      if (t >= p.T) break;
-      const float sum = group_sum<32>(total[t]);
-      if (lane == 0) ((X*)p.y)[(size_t)t * p.H + h] = from_float<X>(sum);
-    }
-  }
+  };
+  down.run(&start, slots, [&](int u, int t) { return s.w[t * p.K + s.pick[u][t]]; }, finish_down);
+  __syncthreads();
+  down.join(slots, finish_down);
 }
 
-static cudaError_t launch_cooperative(void (*kern)(LayerFewParams), int grid, size_t smem, cudaStream_t st, const LayerFewParams& q) {
+template <typename W, int NT>
+static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q, cudaStream_t st) {
+  static SmemAttrOnce once;
+  auto kern = layer_few_kernel<W, NT>;
+  cudaError_t e = ensure_dynamic_smem(kern, RsSizes<W, NT>::BYTES, p->device, once);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = dim3(p->sm_count);
   cfg.blockDim = dim3(kLfThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = RsSizes<W, NT>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
@@ -267,6 +244,10 @@ static cudaError_t launch_cooperative(void (*kern)(LayerFewParams), int grid, si
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
+}
+template <typename W>
+static cudaError_t launch_format(const moe_plan* p, const LayerFewParams& q, cudaStream_t st) {
+  return q.T <= 8 ? launch_cooperative<W, 1>(p, q, st) : launch_cooperative<W, 2>(p, q, st);
 }
 
 // The checks and the launch that both entry points share.
@@ -307,8 +288,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.expert_count = p->s.expert_count;
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
-  auto kern = group > 0 ? layer_few_kernel<W4> : c.dtype == MOE_DTYPE_BF16 ? layer_few_kernel<__nv_bfloat16> : layer_few_kernel<float>;
-  cudaError_t e = launch_cooperative(kern, p->sm_count, 0, st, q);
+  cudaError_t e = group > 0 ? launch_format<W4>(p, q, st) : c.dtype == MOE_DTYPE_BF16 ? launch_format<__nv_bfloat16>(p, q, st) : launch_format<float>(p, q, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     p->cuda_error = (int)e;

@@ -1,0 +1,529 @@
+// Products of matrix rows with a few operand rows ("tokens"), bound by reading the matrix once: what layer_few.cu and w4.cu share.
+//
+// A CTA has a range of matrix rows, cut into tiles of up to 32, and every tile into chunks of columns; its warps take equal,
+// contiguous shares of all (tile, chunk) units, so that they have the same number of bytes to read whatever the sizes are.  Each warp
+// copies its own units into its own ring of shared memory (16-byte asynchronous copies: bytes in flight without registers,
+// no barrier between warps) and multiplies them by the tokens' columns, which come along in the same stage.
+// A tile that lies in one warp's share is finished from registers; of a tile that is cut, the warps after the first leave their
+// sums in shared memory and the first adds them up, in order, so the sum does not depend on timing.
+//
+// The tensor cores' m16n8k16 (mma.sync) forms the products of bf16 and 4-bit rows: sixteen rows by eight tokens costs one
+// instruction per 512 bytes of bf16 weights, so the multiplication is next to free up to 16 tokens, and the fragments come
+// from shared memory without passing through tensor memory, which for tiles this thin would cost more than it gives (tcgen05's
+// smallest tile has 64 rows: more than a CTA's share of the rows of small layers).  fp32 rows take plain FMAs, a lane per row.
+#pragma once
+#include "tc_common.cuh"
+#include "w4_common.cuh"
+
+namespace moehub {
+
+constexpr int kRsThreads = 256;
+constexpr int kRsWarps = kRsThreads / 32;
+constexpr int kRsTile = 32;   // rows of a tile: two runs of up to 16 consecutive rows
+constexpr int kRsRun = 16;
+
+// 16 bytes (or zeros) into shared memory, past L1
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// ---- the weights' formats ----------------------------------------------------------------------------------------------------
+struct W4 {};  // (4 bits; float and __nv_bfloat16 name themselves)
+template <typename W> struct RsFormat;
+template <> struct RsFormat<__nv_bfloat16> {
+  typedef __nv_bfloat16 X;                       // the tokens' type
+  static constexpr int COLS = 64;                // columns of a chunk
+  static constexpr int ROW = 128, XROW = 128;    // their bytes in a weight row, in a token's row
+  static constexpr int SCALES = 0;               // bytes of scales in a stage
+};
+template <> struct RsFormat<float> {
+  typedef float X;
+  static constexpr int COLS = 32, ROW = 128, XROW = 128, SCALES = 0;
+};
+template <> struct RsFormat<W4> {
+  typedef __nv_bfloat16 X;
+  static constexpr int COLS = 128, ROW = 64, XROW = 256;
+  static constexpr int SCALES = 4 * 2 * 9 * 4;   // up to four groups, two runs, nine words (16 scales from an odd one on)
+};
+template <typename W, int NT> struct RsSizes {   // NT: tokens, in eights
+  typedef RsFormat<W> F;
+  static constexpr int A = kRsTile * F::ROW, X = 8 * NT * F::XROW;
+  static constexpr int STAGE = (A + X + F::SCALES + 15) / 16 * 16;
+  static constexpr int REGS = 8 * NT;            // sums per lane
+  static constexpr int SLOTS = kRsWarps * REGS * 32 * 4;
+  static constexpr int ROOM = 219 * 1024 - SLOTS;  // (8 KB are left for the kernels' own tables)
+  static constexpr int STAGES = ROOM / (kRsWarps * STAGE) < 6 ? ROOM / (kRsWarps * STAGE) : 6;
+  static constexpr int RING = kRsWarps * STAGES * STAGE;
+  static constexpr int BYTES = RING + SLOTS;     // dynamic shared memory
+};
+
+// A product's matrix and tokens.  Tokens of matrix number u (a matrix that some token needs) are rows x + u * x_step + t * C.
+struct RsOperand {
+  const void* w0;               // rows of run 0: [matrices, N, C]
+  const void* w1;               // rows of run 1 (gate / up: the other matrix's; else w0)
+  const __nv_bfloat16* s0;      // 4 bits: scales [matrices, C / group, N]
+  const __nv_bfloat16* s1;
+  const void* x;
+  long long x_step;             // elements
+  int N, C, group, matrices;    // matrices: all there are
+};
+
+// The rows of one CTA: [begin, end) of `used` matrices' rows laid end to end.  RT: rows of a tile.
+struct RsRange {
+  long long begin, end;
+  int N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
+  __device__ __forceinline__ RsRange(int used, int N_, int RT_) : N(N_), RT(RT_) {
+    const long long rows = (long long)used * N;
+    begin = rows * blockIdx.x / gridDim.x;
+    end = rows * (blockIdx.x + 1) / gridDim.x;
+    if (end <= begin) { tiles = 0; return; }
+    first_u = (int)(begin / N);
+    first_row = (int)(begin - (long long)first_u * N);
+    first_len = (int)min(end - begin, (long long)(N - first_row));
+    first_tiles = (first_len + RT - 1) / RT;
+    full_tiles = (N + RT - 1) / RT;
+    const int last_u = (int)((end - 1) / N);
+    tiles = first_tiles;
+    if (last_u > first_u) tiles += (last_u - first_u - 1) * full_tiles + (int)(end - (long long)last_u * N + RT - 1) / RT;
+  }
+  // matrix, first row and number of rows of tile i
+  __device__ __forceinline__ void tile(int i, int& u, int& row, int& n) const {
+    int start = first_row, len = first_len, count = first_tiles, k = i;
+    u = first_u;
+    if (i >= first_tiles) {
+      const int j = i - first_tiles, skip = j / full_tiles;
+      u += 1 + skip;
+      k = j - skip * full_tiles;
+      start = 0;
+      len = (int)min((long long)N, end - (long long)u * N);
+      count = (len + RT - 1) / RT;
+    }
+    row = (int)((long long)len * k / count);
+    n = (int)((long long)len * (k + 1) / count) - row;
+    row += start;
+  }
+};
+
+enum RsKind {
+  kRsPairs,   // tiles of up to 16 pairs: row f of w0 and row f of w1, of one matrix each
+  kRsRows,    // tiles of up to 32 rows of one matrix each
+  kRsSum,     // tiles of up to 32 rows, the same rows of every used matrix one after the other, weighted and added
+};
+
+// Which matrices, and which tokens each is for; read from shared memory.
+struct RsList {
+  const int* used;              // matrix of each number
+  const unsigned short* mask;   // tokens of each number
+  int n;
+};
+
+// A warp's way through its units.  KIND as above.
+template <typename W, int NT, int KIND>
+struct RowStream {
+  typedef RsFormat<W> F;
+  typedef RsSizes<W, NT> Z;
+  typedef typename F::X X;
+  static constexpr int REGS = Z::REGS;
+  static constexpr bool kMma = sizeof(X) == 2;
+  static constexpr bool k4Bit = F::SCALES > 0;
+  static constexpr int LPR = F::ROW / 16;         // lanes per weight row of a copy instruction
+  static constexpr int RPI = 32 / LPR;            // rows per instruction
+  static constexpr int XLPR = F::XROW / 16, XRPI = 32 / XLPR;
+
+  const RsOperand& op;
+  const RsList& list;
+  RsRange range;
+  int chunks, per_tile;      // chunks of a matrix row, of a tile
+  long long unit, unit_end;  // what is left to copy, as unit numbers
+  // where the copies are
+  int tile_i, chunk, u, row, n0, n1;  // chunk: of the matrix
+  const char *pa0, *pa1, *px;
+  uint32_t ring;             // shared address of the warp's ring
+  int lane;
+
+  __device__ __forceinline__ RowStream(const RsOperand& op_, const RsList& list_, uint32_t ring_)
+      : op(op_), list(list_), range(KIND == kRsSum ? 1 : list_.n, op_.N, KIND == kRsPairs ? kRsRun : kRsTile), ring(ring_) {
+    lane = threadIdx.x % 32;
+    chunks = (op.C + F::COLS - 1) / F::COLS;
+    per_tile = KIND == kRsSum ? chunks * list.n : chunks;
+    const long long units = (long long)range.tiles * per_tile;
+    const int warp = threadIdx.x / 32;
+    unit = units * warp / kRsWarps;
+    unit_end = units * (warp + 1) / kRsWarps;
+    if (unit < unit_end) {
+      tile_i = (int)(unit / per_tile);
+      const int c = (int)(unit - (long long)tile_i * per_tile);
+      set_tile(tile_i, u, row, n0, n1);
+      if (KIND == kRsSum) u = c / chunks;
+      chunk = KIND == kRsSum ? c - u * chunks : c;
+      set_pointers();
+    }
+  }
+
+  __device__ __forceinline__ void set_tile(int i, int& tu, int& trow, int& tn0, int& tn1) const {
+    int n;
+    range.tile(i, tu, trow, n);
+    if (KIND == kRsPairs) tn0 = tn1 = n;
+    else { tn0 = (n + 1) / 2; tn1 = n - tn0; }
+  }
+  // The second run's first row.
+  __device__ __forceinline__ static int row1(int r, int m0) { return KIND == kRsPairs ? r : r + m0; }
+
+  __device__ __forceinline__ long long row_bytes() const { return k4Bit ? op.C / 2 : (long long)op.C * (int)sizeof(X); }
+  __device__ __forceinline__ void set_pointers() {
+    const long long e = list.used[u], ld = row_bytes();
+    const long long at = (long long)(lane / LPR) * ld + lane % LPR * 16;
+    pa0 = (const char*)op.w0 + (e * op.N + row) * ld + at;
+    pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
+    px = (const char*)op.x + ((long long)u * op.x_step + (long long)(lane / XLPR) * op.C) * (int)sizeof(X) + lane % XLPR * 16;
+  }
+
+  __device__ __forceinline__ void advance() {
+    ++unit;
+    if (++chunk == chunks && unit < unit_end) {
+      chunk = 0;
+      if (KIND == kRsSum && u + 1 < list.n) {
+        ++u;
+      } else {
+        set_tile(++tile_i, u, row, n0, n1);
+        if (KIND == kRsSum) u = 0;
+      }
+      set_pointers();
+    }
+  }
+
+  // The weights (and scales) of the current unit into a stage.
+  __device__ __forceinline__ void copy_weights(int stage) const {
+    const uint32_t dst = ring + stage * Z::STAGE;
+    const long long ld = row_bytes();
+    const int col = chunk * F::ROW + lane % LPR * 16;
+    const bool some = col < ld;
+    const long long off = some ? (long long)chunk * F::ROW : -(lane % LPR * 16);  // (zeros beyond the row: a valid address all the same)
+    const int limit0 = n0 - lane / LPR, limit1 = n1 - lane / LPR;
+#pragma unroll
+    for (int i = 0; i < kRsRun / RPI; ++i) {
+      const int r = i * RPI + lane / LPR;
+      const int unit16 = row_unit(r, lane % LPR);
+      if (i * RPI < limit0) copy16(dst + r * F::ROW + unit16 * 16, pa0 + i * RPI * ld + off, some);
+      if (i * RPI < limit1) copy16(dst + (kRsRun + r) * F::ROW + unit16 * 16, pa1 + i * RPI * ld + off, some);
+    }
+    if constexpr (k4Bit) copy_scales(dst + Z::A + Z::X);
+  }
+  // Shared-memory placement of 16-byte unit c of row r, so that eight rows' same unit lie in different banks.
+  __device__ __forceinline__ static int row_unit(int r, int c) { return F::ROW == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
+  __device__ __forceinline__ static int token_unit(int t, int c) { return F::XROW == 128 ? c ^ (t & 7) : c ^ ((t & 1) << 2); }
+
+  // Scale words: [group of the chunk][run][9], 16 rows from an even element on.
+  __device__ __forceinline__ void copy_scales(uint32_t dst) const {
+    const int per_chunk = F::COLS / op.group, G = op.C / op.group;
+    const long long total = (long long)op.matrices * G * op.N;
+    const long long base = (long long)list.used[u] * G + chunk * per_chunk;
+    for (int w = lane; w < per_chunk * 18; w += 32) {
+      const int q = w / 18, run = w / 9 - 2 * q, i = w % 9;
+      const long long first = (base + q) * op.N + (run == 0 ? row : row1(row, n0));
+      const long long at = (first & ~1ll) + 2 * i;
+      const bool some = chunk * per_chunk + q < G && at < first + (run == 0 ? n0 : n1);
+      const __nv_bfloat16* s = run == 0 ? op.s0 : op.s1;
+      copy4(dst + w * 4, s + (some ? at : 0), some ? (at + 1 < total ? 4 : 2) : 0);
+    }
+  }
+
+  // The tokens' columns of the current unit.
+  __device__ __forceinline__ void copy_tokens(int stage) const {
+    const uint32_t dst = ring + stage * Z::STAGE + Z::A;
+    const unsigned mask = list.mask[u];
+    const int col = chunk * F::XROW + lane % XLPR * 16;
+    const bool some = col < op.C * (int)sizeof(X);
+    const long long off = some ? (long long)chunk * F::XROW : -(lane % XLPR * 16);
+    const long long ld = (long long)op.C * (int)sizeof(X);
+#pragma unroll
+    for (int i = 0; i < 8 * NT / XRPI; ++i) {
+      const int t = i * XRPI + lane / XLPR;
+      if ((mask >> t) & 1u) copy16(dst + t * F::XROW + token_unit(t, lane % XLPR) * 16, px + i * XRPI * ld + off, some);
+    }
+  }
+
+  // One stage's products added to acc.  two: the runs have more than 8 rows.
+  __device__ __forceinline__ void multiply(int stage, unsigned mask, bool two, unsigned scale_parity, float (&acc)[REGS]) const {
+    const uint32_t a = ring + stage * Z::STAGE, x = a + Z::A;
+    if constexpr (!kMma) {
+      float w[32];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + lane * F::ROW + row_unit(lane, c) * 16), w + 4 * c);
+#pragma unroll
+      for (int t = 0; t < 8 * NT; ++t) {
+        if (!((mask >> t) & 1u)) continue;
+        float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          float v[4];
+          Vec16<float>::unpack(lds128(x + t * F::XROW + token_unit(t, c) * 16), v);
+          s0 = __fmaf_rn(w[4 * c], v[0], s0);
+          s1 = __fmaf_rn(w[4 * c + 1], v[1], s1);
+          s0 = __fmaf_rn(w[4 * c + 2], v[2], s0);
+          s1 = __fmaf_rn(w[4 * c + 3], v[3], s1);
+        }
+        acc[t] += s0 + s1;
+      }
+    } else if constexpr (!k4Bit) {
+      uint32_t b[NT][4][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        if (!((mask >> (8 * t)) & 0xffu)) continue;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t r[4];
+          ldsm4(x + (8 * t + lane % 8) * F::XROW + token_unit(lane % 8, 4 * q + lane / 8) * 16, r);
+          b[t][2 * q][0] = r[0]; b[t][2 * q][1] = r[1]; b[t][2 * q + 1][0] = r[2]; b[t][2 * q + 1][1] = r[3];
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (m == 1 && !two) break;
+        const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          uint32_t w[4];
+          ldsm4(a + r * F::ROW + row_unit(r, 2 * k + lane / 16) * 16, w);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if ((mask >> (8 * t)) & 0xffu) mma16816(reinterpret_cast<float(&)[4]>(acc[(m * NT + t) * 4]), w[0], w[1], w[2], w[3], b[t][k][0], b[t][k][1]);
+        }
+      }
+    } else {
+      const uint32_t sc = x + Z::X;
+      const int per_group = op.group / 32;  // 32-column units
+      float part[2][NT][4] = {};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {         // 64 columns each
+        uint32_t w[2][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          if (m == 1 && !two) break;
+          const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
+          ldsm4(a + r * F::ROW + row_unit(r, 2 * h + lane / 16) * 16, w[m]);
+        }
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int k = 2 * h + v;          // 32-column unit
+          uint4 b[NT];
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if ((mask >> (8 * t)) & 0xffu) b[t] = lds128(x + (8 * t + lane / 4) * F::XROW + token_unit(lane / 4, 4 * k + lane % 4) * 16);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            if (m == 1 && !two) break;
+            uint32_t d0[4], d1[4];
+            dequantise(w[m][2 * v], d0);
+            dequantise(w[m][2 * v + 1], d1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+              if ((mask >> (8 * t)) & 0xffu) {
+                mma16816(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t].x, b[t].y);
+                mma16816(part[m][t], d0[2], d1[2], d0[3], d1[3], b[t].z, b[t].w);
+              }
+          }
+          if ((k + 1) % per_group == 0) {   // the group's sums, scaled once
+            const int q = k / per_group;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              if (m == 1 && !two) break;
+              const float f0 = scale(sc, 2 * q, 8 * m + lane / 4 + ((scale_parity >> (2 * q)) & 1));
+              const float f1 = scale(sc, 2 * q + 1, 8 * m + lane / 4 + ((scale_parity >> (2 * q + 1)) & 1));
+#pragma unroll
+              for (int t = 0; t < NT; ++t) {
+                float* s = acc + (m * NT + t) * 4;
+                s[0] = __fmaf_rn(f0, part[m][t][0], s[0]);
+                s[1] = __fmaf_rn(f0, part[m][t][1], s[1]);
+                s[2] = __fmaf_rn(f1, part[m][t][2], s[2]);
+                s[3] = __fmaf_rn(f1, part[m][t][3], s[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[m][t][i] = 0.0f;
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+  // Eight codes as exact bf16 integers code - 8, in pairs of neighbouring columns: 128 + code has the code in its last bits.
+  __device__ __forceinline__ static void dequantise(uint32_t word, uint32_t (&d)[4]) {
+    const __nv_bfloat162 bias = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));  // 136
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t v;
+      asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(v) : "r"(word >> (4 * i)));
+      const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&v), bias);
+      d[i] = *reinterpret_cast<const uint32_t*>(&r);
+    }
+  }
+  __device__ __forceinline__ static float scale(uint32_t sc, int pair, int i) {
+    unsigned short v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(sc + pair * 36 + i * 2) : "memory");
+    return __uint_as_float((uint32_t)v << 16);
+  }
+  // ---- the warp's loop: prefetch() [the weights alone, before the tokens exist], run(), then a barrier of the CTA, then join() ----
+
+  // Where the products are; what run() leaves of a tile that goes on in the next warps' shares.
+  int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_first;
+  bool pending;
+  float sum[REGS];
+
+  __device__ __forceinline__ void prefetch() {
+    __syncwarp();
+#pragma unroll 1
+    for (int i = 0; i < Z::STAGES - 1; ++i)
+      if (unit < unit_end) {
+        copy_weights(i);
+        advance();
+      }
+    copies_commit();
+  }
+
+  // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, t): of a token for a matrix
+  // (kRsSum).  finish(u, row, n0, n1, sums): a whole tile.  slots: shared memory for cut tiles, Z::SLOTS bytes.
+  template <typename Weight, typename Finish>
+  __device__ __forceinline__ void run(RowStream* start, float* slots, Weight weight, Finish finish) {
+    const RowStream& at = start != nullptr ? *start : *this;
+    const int total = (int)(at.unit_end - at.unit);
+    m_tile = at.tile_i; m_u = at.u; m_chunk = at.chunk; m_row = at.row; m_n0 = at.n0; m_n1 = at.n1;
+    pending = false;
+    if (total <= 0) {
+      copies_wait<0>();
+      return;
+    }
+    bool cut = KIND == kRsSum ? m_u != 0 || m_chunk != 0 : m_chunk != 0;  // the tile begins in an earlier warp's share
+#pragma unroll 1
+    for (int i = 0; i < Z::STAGES - 1; ++i) {
+      if (i < total) {
+        if (start != nullptr) {
+          start->copy_tokens(i);
+          start->advance();
+        } else {
+          copy_weights(i);
+          copy_tokens(i);
+          advance();
+        }
+      }
+      copies_commit();
+    }
+    float acc[REGS];
+#pragma unroll
+    for (int j = 0; j < REGS; ++j) acc[j] = sum[j] = 0.0f;
+    int stage = 0, next = Z::STAGES - 1;
+#pragma unroll 1
+    for (int i = 0; i < total; ++i) {
+      __syncwarp();
+      if (unit < unit_end) {
+        copy_weights(next);
+        copy_tokens(next);
+        advance();
+      }
+      copies_commit();
+      copies_wait<Z::STAGES - 1>();
+      __syncwarp();
+      multiply(stage, list.mask[m_u], max(m_n0, m_n1) > 8, parities(m_u, m_chunk, m_row, m_n0), acc);
+      next = stage;
+      stage = stage + 1 == Z::STAGES ? 0 : stage + 1;
+      ++m_chunk;
+      const bool last = i + 1 == total;
+      if (m_chunk < chunks && !last) continue;
+      // the end of a matrix's columns, or of the share
+      if (KIND == kRsSum) {
+        const unsigned mask = list.mask[m_u];
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) {
+          const int t = token(j);
+          if ((mask >> t) & 1u) sum[j] = __fmaf_rn(weight(m_u, t), acc[j], sum[j]);  // (the other tokens' sums hold anything)
+          acc[j] = 0.0f;
+        }
+        if (m_chunk == chunks && m_u + 1 < list.n) {
+          ++m_u;
+          m_chunk = 0;
+          if (!last) continue;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) {
+          sum[j] = acc[j];
+          acc[j] = 0.0f;
+        }
+      }
+      const bool whole = m_chunk == chunks;  // (kRsSum: of the last matrix)
+      if (cut) {
+        float* slot = slots + (threadIdx.x / 32) * (REGS * 32) + lane;
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) slot[j * 32] = sum[j];
+      } else if (whole) {
+        finish(m_u, m_row, m_n0, m_n1, sum);
+      } else {
+        pending = true;
+      }
+      if (!last) {  // (the tile was whole, or its end)
+        cut = false;
+        m_chunk = 0;
+        set_tile(++m_tile, m_u, m_row, m_n0, m_n1);
+        if (KIND == kRsSum) {
+          m_u = 0;
+#pragma unroll
+          for (int j = 0; j < REGS; ++j) sum[j] = 0.0f;
+        }
+      }
+    }
+    copies_wait<0>();
+  }
+
+  // Behind the barrier: the warp that a cut tile begins in adds what the following warps left, and finishes it.
+  template <typename Finish>
+  __device__ __forceinline__ void join(const float* slots, Finish finish) {
+    if (!pending) return;
+    const long long units = (long long)range.tiles * per_tile, tile_end = (long long)(m_tile + 1) * per_tile;
+    for (int w = threadIdx.x / 32 + 1; w < kRsWarps; ++w) {
+      const long long begin = units * w / kRsWarps;
+      if (begin >= tile_end) break;
+      if (units * (w + 1) / kRsWarps == begin) continue;
+      const float* slot = slots + w * (REGS * 32) + lane;
+#pragma unroll
+      for (int j = 0; j < REGS; ++j) sum[j] += slot[j * 32];
+    }
+    finish(m_u, m_row, m_n0, m_n1, sum);
+  }
+
+  // Of sum number j: the token, and (tensor cores) the run, the row in it.
+  __device__ __forceinline__ int token(int j) const { return kMma ? j / 4 % NT * 8 + lane % 4 * 2 + j % 2 : j; }
+  __device__ __forceinline__ int run_of(int j) const { return kMma ? j / 2 % 2 : lane / kRsRun; }
+  __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun; }
+
+  // Which of a chunk's scale words begin one element early: bit 2 * group + run.
+  __device__ __forceinline__ unsigned parities(int mu, int mchunk, int mrow, int m0) const {
+    if constexpr (!k4Bit) return 0;
+    const int per_chunk = F::COLS / op.group, G = op.C / op.group;
+    const unsigned base = (unsigned)list.used[mu] * G + mchunk * per_chunk;
+    unsigned bits = 0;
+    for (int q = 0; q < per_chunk; ++q) {
+      const unsigned first = (base + q) * (unsigned)op.N + mrow;
+      bits |= (first & 1u) << (2 * q) | ((first + (unsigned)(row1(mrow, m0) - mrow)) & 1u) << (2 * q + 1);
+    }
+    return bits;
+  }
+};
+
+}  // namespace moehub

@@ -1,6 +1,6 @@
 // 4-bit weights with group scales: making them from bf16 or fp32 weights, giving them back, and their products with a few
 // rows (moe_w4_pack, moe_w4_unpack, moe_w4_matvec of include/moehub.h).
-#include "w4_common.cuh"
+#include "row_stream.cuh"
 
 namespace moehub {
 
@@ -120,32 +120,75 @@ static cudaError_t launch_unpack(const moe_w4_t& w, size_t words, int N, int C, 
 
 // ---- products with a few rows ------------------------------------------------------------------------------------------------
 
-constexpr int kMatvecThreads = 256;
+constexpr int kMatvecRows = MOE_FEW_MAX_TOKENS;  // at a time
 
-// A warp per result: lanes over the row's words.
-__global__ void __launch_bounds__(kMatvecThreads)
-w4_matvec_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __restrict__ scales, int experts, int N, int C, int G,
-                 const __nv_bfloat16* __restrict__ x, const int* __restrict__ expert, int M, __nv_bfloat16* __restrict__ y) {
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, per_row = C / 8;
-  for (int m = blockIdx.y; m < M; m += gridDim.y) {
-    const int e = expert == nullptr ? 0 : expert[m];
-    if (e < 0 || e >= experts) continue;
-    for (int n = blockIdx.x * (kMatvecThreads / 32) + warp; n < N; n += gridDim.x * (kMatvecThreads / 32)) {
-      float acc = 0.0f;
-      for (int i = lane; i < per_row; i += 32) {
-        const uint32_t word = __ldg(codes + ((size_t)e * N + n) * per_row + i);
-        const float scale = __bfloat162float(scales[((size_t)e * (C / G) + i * 8 / G) * N + n]);
-        float v[8], part = 0.0f;
-        Vec16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(x + (size_t)m * C + i * 8), v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) part = __fmaf_rn(w4_value(word, j), v[j], part);
-        acc = __fmaf_rn(scale, part, acc);
+struct W4MatvecParams {
+  const void* codes;
+  const __nv_bfloat16* scales;
+  const __nv_bfloat16* x;
+  const int* expert;
+  __nv_bfloat16* y;
+  int experts, N, C, group, M;
+};
+
+// Rows of x are taken sixteen (NT 1: eight) at a time; those with the same matrix share its reading.
+template <int NT>
+__global__ void __launch_bounds__(kRsThreads, 1)
+w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
+  typedef RsSizes<W4, NT> Z;
+  extern __shared__ __align__(128) unsigned char dynamic[];
+  __shared__ int used[kMatvecRows], n_used;
+  __shared__ unsigned short mask[kMatvecRows];
+  float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
+  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
+  const int lane = threadIdx.x % 32;
+  for (int m0 = 0; m0 < p.M; m0 += 8 * NT) {
+    const int rows = min(8 * NT, p.M - m0);
+    if (threadIdx.x < 32) {  // the matrices in the order of the first row that wants them
+      int e = lane < rows ? p.expert != nullptr ? p.expert[m0 + lane] : 0 : -1;
+      if (e < 0 || e >= p.experts) e = -1;
+      const unsigned same = __match_any_sync(0xffffffffu, e);
+      const bool first = e >= 0 && lane == __ffs(same) - 1;
+      const unsigned firsts = __ballot_sync(0xffffffffu, first);
+      if (first) {
+        const int at = __popc(firsts & ((1u << lane) - 1u));
+        used[at] = e;
+        mask[at] = (unsigned short)same;
       }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
-      if (lane == 0) y[(size_t)m * N + n] = __float2bfloat16_rn(acc);
+      if (lane == 0) n_used = __popc(firsts);
     }
+    __syncthreads();
+    const RsList list{used, mask, n_used};
+    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.group, p.experts};
+    typedef RowStream<W4, NT, kRsRows> Stream;
+    Stream rs(op, list, ring);
+    auto finish = [&](int u, int row, int n0, int n1, const float (&sum)[Z::REGS]) {
+#pragma unroll
+      for (int j = 0; j < Z::REGS; ++j) {
+        const int t = rs.token(j), r = rs.row_of(j);
+        const bool second = rs.run_of(j) == 1;
+        if (((mask[u] >> t) & 1u) && r < (second ? n1 : n0))
+          p.y[(size_t)(m0 + t) * p.N + row + (second ? n0 : 0) + r] = __float2bfloat16_rn(sum[j]);
+      }
+    };
+    rs.run(nullptr, slots, [](int, int) { return 0.0f; }, finish);
+    __syncthreads();
+    rs.join(slots, finish);
+    __syncthreads();
   }
+}
+
+template <int NT>
+static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
+  static SmemAttrOnce once;
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(w4_matvec_kernel<NT>, RsSizes<W4, NT>::BYTES, device, once);
+  if (e != cudaSuccess) return e;
+  const int sms = sm_count_now();
+  if (sms <= 0) return cudaErrorUnknown;
+  w4_matvec_kernel<NT><<<sms, kRsThreads, RsSizes<W4, NT>::BYTES, st>>>(q);
+  return cudaGetLastError();
 }
 
 }  // namespace moehub
@@ -187,10 +230,8 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
   if (!d_x || !d_y || (experts > 1 && !d_expert)) return MOE_ERR_ARG;
   if (((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) & 15) || (reinterpret_cast<uintptr_t>(d_expert) & 3))
     return MOE_ERR_ALIGN;
-  const dim3 grid(min((N + 7) / 8, 148 * 8), min(M, 65535));
-  w4_matvec_kernel<<<grid, kMatvecThreads, 0, (cudaStream_t)stream>>>((const uint32_t*)w->codes, (const __nv_bfloat16*)w->scales, experts, N, C, group,
-                                                                      (const __nv_bfloat16*)d_x, d_expert, M, (__nv_bfloat16*)d_y);
-  return cudaGetLastError() == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, group, M};
+  return (M <= 8 ? launch_matvec<1>(q, (cudaStream_t)stream) : launch_matvec<2>(q, (cudaStream_t)stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -133,8 +133,14 @@ def test_nan_and_infinity_stay_with_their_token(dtype, group):
     x[7, 511] = float("inf")
     y = torch.zeros_like(want)
     s.call(x=x, y=y)
+    assert y[3].isnan().all() and not y[7].isfinite().all()
+    # The two tokens' picks are others now, so the shares of the warps, and with them the order of a sum, may be: every
+    # other token is held to the definition, by the bound on sums in any order.
     rest = [t for t in range(12) if t not in (3, 7)]
-    assert torch.equal(y[rest], want[rest]) and y[3].isnan().all() and not y[7].isfinite().all()
+    idx = s.plan.layer_tensor(0).long()[rest]
+    logits, dl, _, ref, bound = R.layer(x[rest].double(), s.wr.double(), None, s.matrix(0), s.matrix(1), s.matrix(2), 2, 0, idx, dtype)
+    R.check_picks(idx, logits, dl)
+    R.assert_within(y[rest], ref, bound, "other tokens")
     s.call()
     idx = s.plan.layer_tensor(0).cpu()
     e = int(idx[0, 0])
