@@ -30,7 +30,7 @@ struct LayerFewParams {
   const float* bias;
   LfMatrix wg, wu, wd;
   void* y;
-  int T, H, E, K, F, renorm, group, tp;
+  int T, H, E, K, F, renorm, tp;
   int slices, slice_cols;  // of the router's sums
   float* logits;           // [slices, T, E]
   void* inter;             // [used experts, T, F]
@@ -188,7 +188,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   const RsList list{s.used, s.mask, lf_select(p, s, q)};
 
   // gate and up rows of the used experts
-  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.group, p.E};
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.E};
   typedef RowStream<W, NT, kRsPairs> Up;
   Up up(gate_up, list, ring);
   auto finish_up = [&](int u, int row, int n0, int, const float (&sum)[Z::REGS]) {
@@ -206,7 +206,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   up.run(nullptr, slots, [](int, int) { return 0.0f; }, finish_up);
 
   // the outputs; the first down rows are on their way while the other CTAs finish
-  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, (long long)p.T * p.F, p.H, p.F, p.group, p.E};
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, (long long)p.T * p.F, p.H, p.F, p.E};
   typedef RowStream<W, NT, kRsSum> Down;
   Down down(down_op, list, ring);
   Down start = down;
@@ -273,7 +273,6 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.K = p->route_K;
   q.F = c.F * p->tp;
   q.renorm = c.renormalize;
-  q.group = group;
   q.tp = p->tp;
   // about a task per CTA, no slice under 256 columns; the scratch holds 256 sums per token
   q.slices = max(1, min(min(p->sm_count, 256) / q.E, min(16, c.H / 256)));
@@ -288,7 +287,8 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.expert_count = p->s.expert_count;
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
-  cudaError_t e = group > 0 ? launch_format<W4>(p, q, st) : c.dtype == MOE_DTYPE_BF16 ? launch_format<__nv_bfloat16>(p, q, st) : launch_format<float>(p, q, st);
+  cudaError_t e = group == 32 ? launch_format<W4<32>>(p, q, st) : group == 64 ? launch_format<W4<64>>(p, q, st) : group == 128 ? launch_format<W4<128>>(p, q, st)
+                  : c.dtype == MOE_DTYPE_BF16 ? launch_format<__nv_bfloat16>(p, q, st) : launch_format<float>(p, q, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     p->cuda_error = (int)e;

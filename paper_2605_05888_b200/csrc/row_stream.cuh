@@ -36,7 +36,7 @@ __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
@@ -46,22 +46,22 @@ __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
 }
 
 // ---- the weights' formats ----------------------------------------------------------------------------------------------------
-struct W4 {};  // (4 bits; float and __nv_bfloat16 name themselves)
+template <int GROUP> struct W4 {};  // (4 bits; float and __nv_bfloat16 name themselves)
 template <typename W> struct RsFormat;
 template <> struct RsFormat<__nv_bfloat16> {
   typedef __nv_bfloat16 X;                       // the tokens' type
   static constexpr int COLS = 64;                // columns of a chunk
   static constexpr int ROW = 128, XROW = 128;    // their bytes in a weight row, in a token's row
-  static constexpr int SCALES = 0;               // bytes of scales in a stage
+  static constexpr int SCALES = 0, GROUP = 1, GROUPS = 1;  // bytes of scales in a stage; columns of a group, groups of a chunk
 };
 template <> struct RsFormat<float> {
   typedef float X;
-  static constexpr int COLS = 32, ROW = 128, XROW = 128, SCALES = 0;
+  static constexpr int COLS = 32, ROW = 128, XROW = 128, SCALES = 0, GROUP = 1, GROUPS = 1;
 };
-template <> struct RsFormat<W4> {
+template <int G> struct RsFormat<W4<G>> {
   typedef __nv_bfloat16 X;
-  static constexpr int COLS = 128, ROW = 64, XROW = 256;
-  static constexpr int SCALES = 4 * 2 * 9 * 4;   // up to four groups, two runs, nine words (16 scales from an odd one on)
+  static constexpr int COLS = 128, ROW = 64, XROW = 256, GROUP = G, GROUPS = COLS / G;
+  static constexpr int SCALES = GROUPS * 2 * 9 * 4;  // per group two runs of nine words (16 scales from an odd one on)
 };
 template <typename W, int NT> struct RsSizes {   // NT: tokens, in eights
   typedef RsFormat<W> F;
@@ -83,7 +83,7 @@ struct RsOperand {
   const __nv_bfloat16* s1;
   const void* x;
   long long x_step;             // elements
-  int N, C, group, matrices;    // matrices: all there are
+  int N, C, matrices;           // matrices: all there are
 };
 
 // The rows of one CTA: [begin, end) of `used` matrices' rows laid end to end.  RT: rows of a tile.
@@ -155,7 +155,9 @@ struct RowStream {
   long long unit, unit_end;  // what is left to copy, as unit numbers
   // where the copies are
   int tile_i, chunk, u, row, n0, n1;  // chunk: of the matrix
-  const char *pa0, *pa1, *px;
+  const char *pa0, *pa1, *px;  // the lane's first bytes of the unit
+  long long scale_at;          // (4 bits) the lane's run's first scale of the unit's first group
+  unsigned mask;
   uint32_t ring;             // shared address of the warp's ring
   int lane;
 
@@ -190,14 +192,20 @@ struct RowStream {
   __device__ __forceinline__ long long row_bytes() const { return k4Bit ? op.C / 2 : (long long)op.C * (int)sizeof(X); }
   __device__ __forceinline__ void set_pointers() {
     const long long e = list.used[u], ld = row_bytes();
-    const long long at = (long long)(lane / LPR) * ld + lane % LPR * 16;
+    const long long at = (long long)(lane / LPR) * ld + (long long)chunk * F::ROW + lane % LPR * 16;
     pa0 = (const char*)op.w0 + (e * op.N + row) * ld + at;
     pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
-    px = (const char*)op.x + ((long long)u * op.x_step + (long long)(lane / XLPR) * op.C) * (int)sizeof(X) + lane % XLPR * 16;
+    px = (const char*)op.x + ((long long)u * op.x_step + (long long)(lane / XLPR) * op.C) * (int)sizeof(X) + (long long)chunk * F::XROW + lane % XLPR * 16;
+    mask = list.mask[u];
+    if constexpr (k4Bit) scale_at = (e * (op.C / F::GROUP) + (long long)chunk * F::GROUPS) * op.N + (lane < 16 ? row : row1(row, n0));
   }
 
   __device__ __forceinline__ void advance() {
     ++unit;
+    pa0 += F::ROW;
+    pa1 += F::ROW;
+    px += F::XROW;
+    if constexpr (k4Bit) scale_at += (long long)F::GROUPS * op.N;
     if (++chunk == chunks && unit < unit_end) {
       chunk = 0;
       if (KIND == kRsSum && u + 1 < list.n) {
@@ -213,17 +221,19 @@ struct RowStream {
   // The weights (and scales) of the current unit into a stage.
   __device__ __forceinline__ void copy_weights(int stage) const {
     const uint32_t dst = ring + stage * Z::STAGE;
-    const long long ld = row_bytes();
-    const int col = chunk * F::ROW + lane % LPR * 16;
-    const bool some = col < ld;
-    const long long off = some ? (long long)chunk * F::ROW : -(lane % LPR * 16);  // (zeros beyond the row: a valid address all the same)
+    const long long step = RPI * row_bytes();
+    const bool some = chunk * F::ROW + lane % LPR * 16 < (int)row_bytes();
+    const char *a0 = some ? pa0 : (const char*)op.w0, *a1 = some ? pa1 : (const char*)op.w1;  // (zeros beyond the row)
+    const long long by = some ? step : 0;
     const int limit0 = n0 - lane / LPR, limit1 = n1 - lane / LPR;
 #pragma unroll
     for (int i = 0; i < kRsRun / RPI; ++i) {
       const int r = i * RPI + lane / LPR;
-      const int unit16 = row_unit(r, lane % LPR);
-      if (i * RPI < limit0) copy16(dst + r * F::ROW + unit16 * 16, pa0 + i * RPI * ld + off, some);
-      if (i * RPI < limit1) copy16(dst + (kRsRun + r) * F::ROW + unit16 * 16, pa1 + i * RPI * ld + off, some);
+      const uint32_t at = dst + r * F::ROW + row_unit(r, lane % LPR) * 16;
+      if (i * RPI < limit0) copy16(at, a0, some);
+      if (i * RPI < limit1) copy16(at + kRsRun * F::ROW, a1, some);
+      a0 += by;
+      a1 += by;
     }
     if constexpr (k4Bit) copy_scales(dst + Z::A + Z::X);
   }
@@ -231,38 +241,41 @@ struct RowStream {
   __device__ __forceinline__ static int row_unit(int r, int c) { return F::ROW == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
   __device__ __forceinline__ static int token_unit(int t, int c) { return F::XROW == 128 ? c ^ (t & 7) : c ^ ((t & 1) << 2); }
 
-  // Scale words: [group of the chunk][run][9], 16 rows from an even element on.
+  // Scale words: [group of the chunk][run][9], 16 rows from an even element on; half a warp per run.
   __device__ __forceinline__ void copy_scales(uint32_t dst) const {
-    const int per_chunk = F::COLS / op.group, G = op.C / op.group;
+    const int G = op.C / F::GROUP, i = lane % 16, n = lane < 16 ? n0 : n1;
     const long long total = (long long)op.matrices * G * op.N;
-    const long long base = (long long)list.used[u] * G + chunk * per_chunk;
-    for (int w = lane; w < per_chunk * 18; w += 32) {
-      const int q = w / 18, run = w / 9 - 2 * q, i = w % 9;
-      const long long first = (base + q) * op.N + (run == 0 ? row : row1(row, n0));
+    const __nv_bfloat16* s = lane < 16 ? op.s0 : op.s1;
+    long long first = scale_at;
+#pragma unroll
+    for (int q = 0; q < F::GROUPS; ++q) {
       const long long at = (first & ~1ll) + 2 * i;
-      const bool some = chunk * per_chunk + q < G && at < first + (run == 0 ? n0 : n1);
-      const __nv_bfloat16* s = run == 0 ? op.s0 : op.s1;
-      copy4(dst + w * 4, s + (some ? at : 0), some ? (at + 1 < total ? 4 : 2) : 0);
+      if (i < 9) {
+        const bool some = chunk * F::GROUPS + q < G && 2 * i < n + (int)(first & 1);
+        copy4(dst + (q * 2 + lane / 16) * 36 + i * 4, some ? s + at : s, some ? (at + 1 < total ? 4 : 2) : 0);
+      }
+      first += op.N;
     }
   }
 
   // The tokens' columns of the current unit.
   __device__ __forceinline__ void copy_tokens(int stage) const {
     const uint32_t dst = ring + stage * Z::STAGE + Z::A;
-    const unsigned mask = list.mask[u];
-    const int col = chunk * F::XROW + lane % XLPR * 16;
-    const bool some = col < op.C * (int)sizeof(X);
-    const long long off = some ? (long long)chunk * F::XROW : -(lane % XLPR * 16);
-    const long long ld = (long long)op.C * (int)sizeof(X);
+    const bool some = chunk * F::XROW + lane % XLPR * 16 < op.C * (int)sizeof(X);
+    const long long step = some ? XRPI * (long long)op.C * (int)sizeof(X) : 0;
+    const char* x = some ? px : (const char*)op.x;
+    const unsigned mine = mask >> (lane / XLPR);
 #pragma unroll
     for (int i = 0; i < 8 * NT / XRPI; ++i) {
       const int t = i * XRPI + lane / XLPR;
-      if ((mask >> t) & 1u) copy16(dst + t * F::XROW + token_unit(t, lane % XLPR) * 16, px + i * XRPI * ld + off, some);
+      if ((mine >> (i * XRPI)) & 1u) copy16(dst + t * F::XROW + token_unit(t, lane % XLPR) * 16, x, some);
+      x += step;
     }
   }
 
-  // One stage's products added to acc.  two: the runs have more than 8 rows.
-  __device__ __forceinline__ void multiply(int stage, unsigned mask, bool two, unsigned scale_parity, float (&acc)[REGS]) const {
+  // One stage's products added to acc.  two: the runs have more than 8 rows.  odd0, odd1: bit q, whether the runs' scales of group q
+  // begin in the second half of their first word.
+  __device__ __forceinline__ void multiply(int stage, unsigned mask, bool two, unsigned odd0, unsigned odd1, float (&acc)[REGS]) const {
     const uint32_t a = ring + stage * Z::STAGE, x = a + Z::A;
     if constexpr (!kMma) {
       float w[32];
@@ -310,8 +323,8 @@ struct RowStream {
       }
     } else {
       const uint32_t sc = x + Z::X;
-      const int per_group = op.group / 32;  // 32-column units
-      float part[2][NT][4] = {};
+      constexpr int per_group = F::GROUP / 32;  // 32-column units
+      float part[2][NT][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {         // 64 columns each
         uint32_t w[2][4];
@@ -324,6 +337,10 @@ struct RowStream {
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           const int k = 2 * h + v;          // 32-column unit
+          if (k % per_group == 0) {
+#pragma unroll
+            for (int j = 0; j < 8 * NT; ++j) part[j / (4 * NT)][j / 4 % NT][j % 4] = 0.0f;
+          }
           uint4 b[NT];
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -346,8 +363,8 @@ struct RowStream {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
               if (m == 1 && !two) break;
-              const float f0 = scale(sc, 2 * q, 8 * m + lane / 4 + ((scale_parity >> (2 * q)) & 1));
-              const float f1 = scale(sc, 2 * q + 1, 8 * m + lane / 4 + ((scale_parity >> (2 * q + 1)) & 1));
+              const float f0 = scale(sc, 2 * q, 8 * m + lane / 4 + ((odd0 >> q) & 1));
+              const float f1 = scale(sc, 2 * q + 1, 8 * m + lane / 4 + ((odd1 >> q) & 1));
 #pragma unroll
               for (int t = 0; t < NT; ++t) {
                 float* s = acc + (m * NT + t) * 4;
@@ -355,8 +372,6 @@ struct RowStream {
                 s[1] = __fmaf_rn(f0, part[m][t][1], s[1]);
                 s[2] = __fmaf_rn(f1, part[m][t][2], s[2]);
                 s[3] = __fmaf_rn(f1, part[m][t][3], s[3]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[m][t][i] = 0.0f;
               }
             }
           }
@@ -383,7 +398,8 @@ struct RowStream {
   // ---- the warp's loop: prefetch() [the weights alone, before the tokens exist], run(), then a barrier of the CTA, then join() ----
 
   // Where the products are; what run() leaves of a tile that goes on in the next warps' shares.
-  int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_first;
+  int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_base;
+  unsigned m_mask;
   bool pending;
   float sum[REGS];
 
@@ -398,6 +414,11 @@ struct RowStream {
     copies_commit();
   }
 
+  __device__ __forceinline__ void set_matrix() {
+    m_mask = list.mask[m_u];
+    if constexpr (k4Bit) m_base = list.used[m_u] * (op.C / F::GROUP);
+  }
+
   // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, t): of a token for a matrix
   // (kRsSum).  finish(u, row, n0, n1, sums): a whole tile.  slots: shared memory for cut tiles, Z::SLOTS bytes.
   template <typename Weight, typename Finish>
@@ -410,6 +431,7 @@ struct RowStream {
       copies_wait<0>();
       return;
     }
+    set_matrix();
     bool cut = KIND == kRsSum ? m_u != 0 || m_chunk != 0 : m_chunk != 0;  // the tile begins in an earlier warp's share
 #pragma unroll 1
     for (int i = 0; i < Z::STAGES - 1; ++i) {
@@ -440,7 +462,13 @@ struct RowStream {
       copies_commit();
       copies_wait<Z::STAGES - 1>();
       __syncwarp();
-      multiply(stage, list.mask[m_u], max(m_n0, m_n1) > 8, parities(m_u, m_chunk, m_row, m_n0), acc);
+      unsigned odd0 = 0, odd1 = 0;
+      if constexpr (k4Bit) {  // scale number (matrix's + group) * N + row
+        const unsigned swing = op.N & 1 ? 0xau ^ ((m_base + m_chunk * F::GROUPS) & 1 ? 0xfu : 0u) : 0u;
+        odd0 = swing ^ (m_row & 1 ? 0xfu : 0u);
+        odd1 = swing ^ (row1(m_row, m_n0) & 1 ? 0xfu : 0u);
+      }
+      multiply(stage, m_mask, m_n0 > 8, odd0, odd1, acc);
       next = stage;
       stage = stage + 1 == Z::STAGES ? 0 : stage + 1;
       ++m_chunk;
@@ -448,16 +476,16 @@ struct RowStream {
       if (m_chunk < chunks && !last) continue;
       // the end of a matrix's columns, or of the share
       if (KIND == kRsSum) {
-        const unsigned mask = list.mask[m_u];
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
           const int t = token(j);
-          if ((mask >> t) & 1u) sum[j] = __fmaf_rn(weight(m_u, t), acc[j], sum[j]);  // (the other tokens' sums hold anything)
+          if ((m_mask >> t) & 1u) sum[j] = __fmaf_rn(weight(m_u, t), acc[j], sum[j]);  // (the other tokens' sums hold anything)
           acc[j] = 0.0f;
         }
         if (m_chunk == chunks && m_u + 1 < list.n) {
           ++m_u;
           m_chunk = 0;
+          set_matrix();
           if (!last) continue;
         }
       } else {
@@ -486,6 +514,7 @@ struct RowStream {
 #pragma unroll
           for (int j = 0; j < REGS; ++j) sum[j] = 0.0f;
         }
+        set_matrix();
       }
     }
     copies_wait<0>();
@@ -511,19 +540,6 @@ struct RowStream {
   __device__ __forceinline__ int token(int j) const { return kMma ? j / 4 % NT * 8 + lane % 4 * 2 + j % 2 : j; }
   __device__ __forceinline__ int run_of(int j) const { return kMma ? j / 2 % 2 : lane / kRsRun; }
   __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun; }
-
-  // Which of a chunk's scale words begin one element early: bit 2 * group + run.
-  __device__ __forceinline__ unsigned parities(int mu, int mchunk, int mrow, int m0) const {
-    if constexpr (!k4Bit) return 0;
-    const int per_chunk = F::COLS / op.group, G = op.C / op.group;
-    const unsigned base = (unsigned)list.used[mu] * G + mchunk * per_chunk;
-    unsigned bits = 0;
-    for (int q = 0; q < per_chunk; ++q) {
-      const unsigned first = (base + q) * (unsigned)op.N + mrow;
-      bits |= (first & 1u) << (2 * q) | ((first + (unsigned)(row1(mrow, m0) - mrow)) & 1u) << (2 * q + 1);
-    }
-    return bits;
-  }
 };
 
 }  // namespace moehub

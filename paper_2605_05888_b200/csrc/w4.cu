@@ -128,14 +128,14 @@ struct W4MatvecParams {
   const __nv_bfloat16* x;
   const int* expert;
   __nv_bfloat16* y;
-  int experts, N, C, group, M;
+  int experts, N, C, M;
 };
 
 // Rows of x are taken sixteen (NT 1: eight) at a time; those with the same matrix share its reading.
-template <int NT>
+template <int G, int NT>
 __global__ void __launch_bounds__(kRsThreads, 1)
 w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
-  typedef RsSizes<W4, NT> Z;
+  typedef RsSizes<W4<G>, NT> Z;
   extern __shared__ __align__(128) unsigned char dynamic[];
   __shared__ int used[kMatvecRows], n_used;
   __shared__ unsigned short mask[kMatvecRows];
@@ -159,8 +159,8 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
     }
     __syncthreads();
     const RsList list{used, mask, n_used};
-    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.group, p.experts};
-    typedef RowStream<W4, NT, kRsRows> Stream;
+    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts};
+    typedef RowStream<W4<G>, NT, kRsRows> Stream;
     Stream rs(op, list, ring);
     auto finish = [&](int u, int row, int n0, int n1, const float (&sum)[Z::REGS]) {
 #pragma unroll
@@ -178,16 +178,16 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
   }
 }
 
-template <int NT>
+template <int G, int NT>
 static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   static SmemAttrOnce once;
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
-  if (e == cudaSuccess) e = ensure_dynamic_smem(w4_matvec_kernel<NT>, RsSizes<W4, NT>::BYTES, device, once);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(w4_matvec_kernel<G, NT>, RsSizes<W4<G>, NT>::BYTES, device, once);
   if (e != cudaSuccess) return e;
   const int sms = sm_count_now();
   if (sms <= 0) return cudaErrorUnknown;
-  w4_matvec_kernel<NT><<<sms, kRsThreads, RsSizes<W4, NT>::BYTES, st>>>(q);
+  w4_matvec_kernel<G, NT><<<sms, kRsThreads, RsSizes<W4<G>, NT>::BYTES, st>>>(q);
   return cudaGetLastError();
 }
 
@@ -230,8 +230,12 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
   if (!d_x || !d_y || (experts > 1 && !d_expert)) return MOE_ERR_ARG;
   if (((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) & 15) || (reinterpret_cast<uintptr_t>(d_expert) & 3))
     return MOE_ERR_ALIGN;
-  const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, group, M};
-  return (M <= 8 ? launch_matvec<1>(q, (cudaStream_t)stream) : launch_matvec<2>(q, (cudaStream_t)stream)) == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
+  const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, M};
+  cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e;
+  if (M <= 8) e = group == 32 ? launch_matvec<32, 1>(q, st) : group == 64 ? launch_matvec<64, 1>(q, st) : launch_matvec<128, 1>(q, st);
+  else e = group == 32 ? launch_matvec<32, 2>(q, st) : group == 64 ? launch_matvec<64, 2>(q, st) : launch_matvec<128, 2>(q, st);
+  return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
 }  // extern "C"
