@@ -13,11 +13,9 @@
 
 namespace moehub {
 
-constexpr int kLfThreads = kRsThreads;
-constexpr int kLfWarps = kRsWarps;
+constexpr int kLfMaxWarps = 16;
 constexpr int kLfTokens = MOE_FEW_MAX_TOKENS;
 constexpr int kLfPicks = 32;  // most picks per token
-static_assert(kMaxExperts == kLfThreads, "a thread per expert");
 
 struct LfMatrix {
   const void* w;                // [E, N, C] of the weights' type, or the codes
@@ -74,10 +72,10 @@ struct LfShared {
   int used[kMaxExperts];                       // the used experts, ascending
   unsigned short mask[kMaxExperts];            // the tokens that picked each
   unsigned char pick[kMaxExperts][kLfTokens];  // which of its picks the expert is for a token
-  int warp_used[kLfWarps];
+  int warp_used[kMaxExperts / 32];
 };
 struct LfSelect {  // where the rows are streamed through later
-  float red[kLfWarps][kLfTokens];
+  float red[kLfMaxWarps][kLfTokens];
   int idx[kLfTokens * kLfPicks];
   unsigned mask[kMaxExperts];
   int pos[kMaxExperts];  // a used expert's number
@@ -93,7 +91,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     const int e = task / p.slices, slice = task % p.slices;
     const int c0 = slice * p.slice_cols, c1 = min(p.H, c0 + p.slice_cols);
     float acc[kLfTokens] = {};
-    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += kLfThreads * N) {
+    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += blockDim.x * N) {
       float w[N];
       Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)e * p.H + c), w);
 #pragma unroll
@@ -116,7 +114,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     if ((int)threadIdx.x < p.T) {
       float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kLfWarps; ++i) sum += s.red[i][threadIdx.x];
+      for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += s.red[i][threadIdx.x];
       __stcg(p.logits + ((size_t)slice * p.T + threadIdx.x) * p.E + e, sum);
     }
     __syncthreads();
@@ -126,17 +124,17 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
 // Every CTA selects for itself; returns the number of used experts.
 __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  for (int i = tid; i < p.T * p.E; i += kLfThreads) {
+  for (int i = tid; i < p.T * p.E; i += blockDim.x) {
     float sum = 0.0f;
     for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
     q.logits[i] = p.bias != nullptr ? sum + p.bias[i % p.E] : sum;
   }
-  q.mask[tid] = 0;
+  if (tid < kMaxExperts) q.mask[tid] = 0;
   __syncthreads();
   if (p.E <= 64) select_topk<32, 2>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   else select_topk<32, 8>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
+  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
     atomicOr(&q.mask[q.idx[a]], 1u << (a / p.K));
     if (blockIdx.x == 0)
       for (int sh = 0; sh < p.tp; ++sh) {
@@ -145,26 +143,26 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
       }
   }
   __syncthreads();
-  const bool mine = q.mask[tid] != 0;
+  const bool mine = tid < kMaxExperts && q.mask[tid] != 0;
   if (blockIdx.x == 0)
-    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(q.mask[e / p.tp]);
+    for (int e = tid; e < p.E * p.tp; e += blockDim.x) p.expert_count[e] = __popc(q.mask[e / p.tp]);
   const unsigned b = __ballot_sync(0xffffffffu, mine);
-  if (lane == 0) s.warp_used[warp] = __popc(b);
+  if (lane == 0 && tid < kMaxExperts) s.warp_used[warp] = __popc(b);
   __syncthreads();
   int before = 0, n = 0;
 #pragma unroll
-  for (int i = 0; i < kLfWarps; ++i) {
+  for (int i = 0; i < kMaxExperts / 32; ++i) {
     if (i < warp) before += s.warp_used[i];
     n += s.warp_used[i];
   }
   const int pos = before + __popc(b & ((1u << lane) - 1u));
-  q.pos[tid] = pos;
+  if (tid < kMaxExperts) q.pos[tid] = pos;
   if (mine) {
     s.used[pos] = tid;
     s.mask[pos] = (unsigned short)q.mask[tid];
   }
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += kLfThreads) s.pick[q.pos[q.idx[a]]][a / p.K] = (unsigned char)(a % p.K);
+  for (int a = tid; a < p.T * p.K; a += blockDim.x) s.pick[q.pos[q.idx[a]]][a / p.K] = (unsigned char)(a % p.K);
   __syncthreads();
   return n;
 }
@@ -172,7 +170,7 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
 template <typename W, int NT>
-__global__ void __launch_bounds__(kLfThreads, 1)
+__global__ void __launch_bounds__(RsSizes<W, NT>::THREADS, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   typedef typename RsFormat<W>::X X;
   typedef RsSizes<W, NT> Z;
@@ -235,7 +233,7 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p->sm_count);
-  cfg.blockDim = dim3(kLfThreads);
+  cfg.blockDim = dim3(RsSizes<W, NT>::THREADS);
   cfg.dynamicSmemBytes = RsSizes<W, NT>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

@@ -17,8 +17,6 @@
 
 namespace moehub {
 
-constexpr int kRsThreads = 256;
-constexpr int kRsWarps = kRsThreads / 32;
 constexpr int kRsTile = 32;   // rows of a tile: two runs of up to 16 consecutive rows
 constexpr int kRsRun = 16;
 
@@ -68,10 +66,11 @@ template <typename W, int NT> struct RsSizes {   // NT: tokens, in eights
   static constexpr int A = kRsTile * F::ROW, X = 8 * NT * F::XROW;
   static constexpr int STAGE = (A + X + F::SCALES + 15) / 16 * 16;
   static constexpr int REGS = 8 * NT;            // sums per lane
-  static constexpr int SLOTS = kRsWarps * REGS * 32 * 4;
+  static constexpr int WARPS = F::SCALES > 0 ? 16 : 8, THREADS = 32 * WARPS;
+  static constexpr int SLOTS = WARPS * REGS * 32 * 4;
   static constexpr int ROOM = 219 * 1024 - SLOTS;  // (8 KB are left for the kernels' own tables)
-  static constexpr int STAGES = ROOM / (kRsWarps * STAGE) < 6 ? ROOM / (kRsWarps * STAGE) : 6;
-  static constexpr int RING = kRsWarps * STAGES * STAGE;
+  static constexpr int STAGES = ROOM / (WARPS * STAGE) < 6 ? ROOM / (WARPS * STAGE) : 6;
+  static constexpr int RING = WARPS * STAGES * STAGE;
   static constexpr int BYTES = RING + SLOTS;     // dynamic shared memory
 };
 
@@ -141,7 +140,7 @@ struct RowStream {
   typedef RsFormat<W> F;
   typedef RsSizes<W, NT> Z;
   typedef typename F::X X;
-  static constexpr int REGS = Z::REGS;
+  static constexpr int REGS = Z::REGS, WARPS = Z::WARPS;
   static constexpr bool kMma = sizeof(X) == 2;
   static constexpr bool k4Bit = F::SCALES > 0;
   static constexpr int LPR = F::ROW / 16;         // lanes per weight row of a copy instruction
@@ -168,8 +167,8 @@ struct RowStream {
     per_tile = KIND == kRsSum ? chunks * list.n : chunks;
     const long long units = (long long)range.tiles * per_tile;
     const int warp = threadIdx.x / 32;
-    unit = units * warp / kRsWarps;
-    unit_end = units * (warp + 1) / kRsWarps;
+    unit = units * warp / WARPS;
+    unit_end = units * (warp + 1) / WARPS;
     if (unit < unit_end) {
       tile_i = (int)(unit / per_tile);
       const int c = (int)(unit - (long long)tile_i * per_tile);
@@ -525,10 +524,10 @@ struct RowStream {
   __device__ __forceinline__ void join(const float* slots, Finish finish) {
     if (!pending) return;
     const long long units = (long long)range.tiles * per_tile, tile_end = (long long)(m_tile + 1) * per_tile;
-    for (int w = threadIdx.x / 32 + 1; w < kRsWarps; ++w) {
-      const long long begin = units * w / kRsWarps;
+    for (int w = threadIdx.x / 32 + 1; w < WARPS; ++w) {
+      const long long begin = units * w / WARPS;
       if (begin >= tile_end) break;
-      if (units * (w + 1) / kRsWarps == begin) continue;
+      if (units * (w + 1) / WARPS == begin) continue;
       const float* slot = slots + w * (REGS * 32) + lane;
 #pragma unroll
       for (int j = 0; j < REGS; ++j) sum[j] += slot[j * 32];

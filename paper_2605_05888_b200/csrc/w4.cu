@@ -133,7 +133,7 @@ struct W4MatvecParams {
 
 // Rows of x are taken sixteen (NT 1: eight) at a time; those with the same matrix share its reading.
 template <int G, int NT>
-__global__ void __launch_bounds__(kRsThreads, 1)
+__global__ void __launch_bounds__(RsSizes<W4<G>, NT>::THREADS, 1)
 w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
   typedef RsSizes<W4<G>, NT> Z;
   extern __shared__ __align__(128) unsigned char dynamic[];
@@ -187,7 +187,7 @@ static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int sms = sm_count_now();
   if (sms <= 0) return cudaErrorUnknown;
-  w4_matvec_kernel<G, NT><<<sms, kRsThreads, RsSizes<W4<G>, NT>::BYTES, st>>>(q);
+  w4_matvec_kernel<G, NT><<<sms, RsSizes<W4<G>, NT>::THREADS, RsSizes<W4<G>, NT>::BYTES, st>>>(q);
   return cudaGetLastError();
 }
 
