@@ -13,7 +13,9 @@
 
 namespace moehub {
 
-constexpr int kLfMaxWarps = 16;
+constexpr int kLfThreads = 256;
+constexpr int kLfWarps = kLfThreads / 32;
+static_assert(kMaxExperts == kLfThreads, "a thread per expert");
 constexpr int kLfTokens = MOE_FEW_MAX_TOKENS;
 constexpr int kLfPicks = 32;  // most picks per token
 
@@ -31,7 +33,7 @@ struct LayerFewParams {
   int T, H, E, K, F, renorm, tp;
   int slices, slice_cols;  // of the router's sums
   float* logits;           // [slices, T, E]
-  void* inter;             // [used experts, T, F]
+  void* inter;             // [entries, 8, F]: the gate / up results of an entry's tokens
   unsigned* sync;          // two barriers: {arrived, generation} each
   int* topk_idx;           // the picks and rows per expert, as moe_layer leaves them (every TP shard listed)
   float* topk_w;
@@ -67,18 +69,21 @@ __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which)
   __syncthreads();
 }
 
+constexpr int kLfSlots = 8;      // tokens of an entry
+constexpr int kLfEntries = 320;  // most entries: 256 experts, and 32 more eights of tokens among sixteen times 32 picks
 struct LfShared {
-  float w[kLfTokens * kLfPicks];               // the picks' weights
-  int used[kMaxExperts];                       // the used experts, ascending
-  unsigned short mask[kMaxExperts];            // the tokens that picked each
-  unsigned char pick[kMaxExperts][kLfTokens];  // which of its picks the expert is for a token
+  float w[kLfTokens * kLfPicks];                    // the picks' weights
+  unsigned short used[kLfEntries];                  // an entry's expert, ascending
+  unsigned char count[kLfEntries];
+  unsigned char token[kLfEntries * kLfSlots];       // its tokens
+  unsigned char pick[kLfEntries * kLfSlots];        // and which of a token's picks it is
   int warp_used[kMaxExperts / 32];
 };
 struct LfSelect {  // where the rows are streamed through later
-  float red[kLfMaxWarps][kLfTokens];
+  float red[kLfWarps][kLfTokens];
   int idx[kLfTokens * kLfPicks];
   unsigned mask[kMaxExperts];
-  int pos[kMaxExperts];  // a used expert's number
+  int pos[kMaxExperts];  // a used expert's first entry
   float logits[kLfTokens * kMaxExperts];
 };
 
@@ -91,7 +96,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     const int e = task / p.slices, slice = task % p.slices;
     const int c0 = slice * p.slice_cols, c1 = min(p.H, c0 + p.slice_cols);
     float acc[kLfTokens] = {};
-    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += blockDim.x * N) {
+    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += kLfThreads * N) {
       float w[N];
       Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)e * p.H + c), w);
 #pragma unroll
@@ -114,17 +119,17 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     if ((int)threadIdx.x < p.T) {
       float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += s.red[i][threadIdx.x];
+      for (int i = 0; i < (int)kLfWarps; ++i) sum += s.red[i][threadIdx.x];
       __stcg(p.logits + ((size_t)slice * p.T + threadIdx.x) * p.E + e, sum);
     }
     __syncthreads();
   }
 }
 
-// Every CTA selects for itself; returns the number of used experts.
+// Every CTA selects for itself; returns the number of entries.
 __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  for (int i = tid; i < p.T * p.E; i += blockDim.x) {
+  for (int i = tid; i < p.T * p.E; i += kLfThreads) {
     float sum = 0.0f;
     for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
     q.logits[i] = p.bias != nullptr ? sum + p.bias[i % p.E] : sum;
@@ -134,7 +139,7 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
   if (p.E <= 64) select_topk<32, 2>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   else select_topk<32, 8>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
+  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
     atomicOr(&q.mask[q.idx[a]], 1u << (a / p.K));
     if (blockIdx.x == 0)
       for (int sh = 0; sh < p.tp; ++sh) {
@@ -143,98 +148,103 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
       }
   }
   __syncthreads();
-  const bool mine = tid < kMaxExperts && q.mask[tid] != 0;
   if (blockIdx.x == 0)
-    for (int e = tid; e < p.E * p.tp; e += blockDim.x) p.expert_count[e] = __popc(q.mask[e / p.tp]);
-  const unsigned b = __ballot_sync(0xffffffffu, mine);
-  if (lane == 0 && tid < kMaxExperts) s.warp_used[warp] = __popc(b);
+    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(q.mask[e / p.tp]);
+  // entries: one per used expert and eight tokens of it
+  const int tokens = __popc(q.mask[tid]), entries = (tokens + kLfSlots - 1) / kLfSlots;
+  int upto = entries;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, upto, off);
+    if (lane >= off) upto += v;
+  }
+  if (lane == 31) s.warp_used[warp] = upto;
   __syncthreads();
-  int before = 0, n = 0;
+  int pos = upto - entries, n = 0;
 #pragma unroll
   for (int i = 0; i < kMaxExperts / 32; ++i) {
-    if (i < warp) before += s.warp_used[i];
+    if (i < warp) pos += s.warp_used[i];
     n += s.warp_used[i];
   }
-  const int pos = before + __popc(b & ((1u << lane) - 1u));
-  if (tid < kMaxExperts) q.pos[tid] = pos;
-  if (mine) {
-    s.used[pos] = tid;
-    s.mask[pos] = (unsigned short)q.mask[tid];
+  q.pos[tid] = pos;
+  for (int i = 0; i < entries; ++i) {
+    s.used[pos + i] = (unsigned short)tid;
+    s.count[pos + i] = (unsigned char)min(kLfSlots, tokens - i * kLfSlots);
   }
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += blockDim.x) s.pick[q.pos[q.idx[a]]][a / p.K] = (unsigned char)(a % p.K);
+  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
+    const int t = a / p.K, e = q.idx[a], slot = q.pos[e] * kLfSlots + __popc(q.mask[e] & ((1u << t) - 1u));
+    s.token[slot] = (unsigned char)t;
+    s.pick[slot] = (unsigned char)(a % p.K);
+  }
   __syncthreads();
   return n;
 }
 
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
-template <typename W, int NT>
-__global__ void __launch_bounds__(RsSizes<W, NT>::THREADS, 1)
+template <typename W>
+__global__ void __launch_bounds__(kLfThreads, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   typedef typename RsFormat<W>::X X;
-  typedef RsSizes<W, NT> Z;
+  typedef RsSizes<W, 1> Z;
   extern __shared__ __align__(128) unsigned char dynamic[];
   __shared__ LfShared s;
-  static_assert(sizeof(LfSelect) <= Z::RING, "the selection's tables lie in the ring");
+  static_assert(sizeof(LfSelect) <= Z::RING && Z::THREADS == kLfThreads, "the selection's tables lie in the ring");
   LfSelect& q = *reinterpret_cast<LfSelect*>(dynamic);
   float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
   const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
+  const int lane = threadIdx.x % 32;
   if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
   lf_router<X>(p, q);
   grid_barrier(p, 0);
-  const RsList list{s.used, s.mask, lf_select(p, s, q)};
+  const RsList list{s.used, s.count, s.token, lf_select(p, s, q)};
 
   // gate and up rows of the used experts
-  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.E};
-  typedef RowStream<W, NT, kRsPairs> Up;
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, p.F, p.H, p.E};
+  typedef RowStream<W, 1, kRsPairs> Up;
   Up up(gate_up, list, ring);
-  auto finish_up = [&](int u, int row, int n0, int, const float (&sum)[Z::REGS]) {
-    const unsigned mask = s.mask[u];
+  auto finish_up = [&](int u, int row, int n0, int, const float*) {
 #pragma unroll
     for (int j = 0; j < Z::REGS; ++j) {
+      if (Up::kMma && j % 4 >= 2) continue;
+      const float upper = Up::kMma ? up.acc[Up::kMma ? j + 2 : j] : __shfl_down_sync(0xffffffffu, up.acc[j], kRsRun);
       const int t = up.token(j), f = up.row_of(j);
-      float v = 0.0f;
-      if (Up::kMma && j % 4 < 2) v = lf_silu_mul(sum[j], sum[Up::kMma ? j + 2 : j]);
-      if (!Up::kMma) v = lf_silu_mul(sum[j], __shfl_down_sync(0xffffffffu, sum[j], kRsRun));
-      if ((Up::kMma ? j % 4 < 2 : threadIdx.x % 32 < kRsRun) && f < n0 && ((mask >> t) & 1u))
-        ((X*)p.inter)[((size_t)u * p.T + t) * p.F + row + f] = from_float<X>(v);
+      if (t < s.count[u] && f < n0 && (Up::kMma || lane < kRsRun))
+        ((X*)p.inter)[((size_t)u * kLfSlots + t) * p.F + row + f] = from_float<X>(lf_silu_mul(up.acc[j], upper));
     }
   };
   up.run(nullptr, slots, [](int, int) { return 0.0f; }, finish_up);
 
   // the outputs; the first down rows are on their way while the other CTAs finish
-  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, (long long)p.T * p.F, p.H, p.F, p.E};
-  typedef RowStream<W, NT, kRsSum> Down;
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, p.H, p.F, p.E};
+  typedef RowStream<W, 1, kRsSum> Down;
   Down down(down_op, list, ring);
   Down start = down;
   down.prefetch();
   __syncthreads();
   up.join(slots, finish_up);
   grid_barrier(p, 1);
-  auto finish_down = [&](int, int row, int n0, int n1, const float (&sum)[Z::REGS]) {
-#pragma unroll
-    for (int j = 0; j < Z::REGS; ++j) {
-      const int t = down.token(j), r = down.row_of(j);
-      const bool second = down.run_of(j) == 1;
-      if (t < p.T && r < (second ? n1 : n0)) ((X*)p.y)[(size_t)t * p.H + row + (second ? n0 : 0) + r] = from_float<X>(sum[j]);
-    }
+  auto finish_down = [&](int, int row, int n0, int n1, const float* sums) {
+    const int r = lane % kRsRun, first = lane < kRsRun ? row : row + n0;
+    if (r < (lane < kRsRun ? n0 : n1))
+      for (int t = 0; t < p.T; ++t) ((X*)p.y)[(size_t)t * p.H + first + r] = from_float<X>(sums[Down::sum_at(t, lane)]);
   };
-  down.run(&start, slots, [&](int u, int t) { return s.w[t * p.K + s.pick[u][t]]; }, finish_down);
+  down.run(&start, slots, [&](int u, int slot) { return s.w[s.token[u * kLfSlots + slot] * p.K + s.pick[u * kLfSlots + slot]]; }, finish_down);
   __syncthreads();
   down.join(slots, finish_down);
 }
 
-template <typename W, int NT>
+template <typename W>
 static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q, cudaStream_t st) {
   static SmemAttrOnce once;
-  auto kern = layer_few_kernel<W, NT>;
-  cudaError_t e = ensure_dynamic_smem(kern, RsSizes<W, NT>::BYTES, p->device, once);
+  auto kern = layer_few_kernel<W>;
+  cudaError_t e = ensure_dynamic_smem(kern, RsSizes<W, 1>::BYTES, p->device, once);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p->sm_count);
-  cfg.blockDim = dim3(RsSizes<W, NT>::THREADS);
-  cfg.dynamicSmemBytes = RsSizes<W, NT>::BYTES;
+  cfg.blockDim = dim3(kLfThreads);
+  cfg.dynamicSmemBytes = RsSizes<W, 1>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeCooperative;
@@ -243,11 +253,6 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
 }
-template <typename W>
-static cudaError_t launch_format(const moe_plan* p, const LayerFewParams& q, cudaStream_t st) {
-  return q.T <= 8 ? launch_cooperative<W, 1>(p, q, st) : launch_cooperative<W, 2>(p, q, st);
-}
-
 // The checks and the launch that both entry points share.
 static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bias, LfMatrix wg, LfMatrix wu, LfMatrix wd, int group,
                      void* y, cudaStream_t st) {
@@ -257,6 +262,9 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess) return MOE_ERR_CUDA;
   if (device != p->device) return MOE_ERR_ARG;
+  // the tokens' rows, and the gate / up results of at most two entries per expert, have 32-bit offsets
+  const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
+  if (c.T * c.H * eb >= 1ll << 32 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 32) return MOE_ERR_UNSUPPORTED;
   LayerFewParams q = {};
   q.x = x;
   q.wr = wr;
@@ -285,8 +293,8 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.expert_count = p->s.expert_count;
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
-  cudaError_t e = group == 32 ? launch_format<W4<32>>(p, q, st) : group == 64 ? launch_format<W4<64>>(p, q, st) : group == 128 ? launch_format<W4<128>>(p, q, st)
-                  : c.dtype == MOE_DTYPE_BF16 ? launch_format<__nv_bfloat16>(p, q, st) : launch_format<float>(p, q, st);
+  cudaError_t e = group == 32 ? launch_cooperative<W4<32>>(p, q, st) : group == 64 ? launch_cooperative<W4<64>>(p, q, st) : group == 128 ? launch_cooperative<W4<128>>(p, q, st)
+                  : c.dtype == MOE_DTYPE_BF16 ? launch_cooperative<__nv_bfloat16>(p, q, st) : launch_cooperative<float>(p, q, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     p->cuda_error = (int)e;

@@ -8,7 +8,7 @@
 // sums in shared memory and the first adds them up, in order, so the sum does not depend on timing.
 //
 // The tensor cores' m16n8k16 (mma.sync) forms the products of bf16 and 4-bit rows: sixteen rows by eight tokens costs one
-// instruction per 512 bytes of bf16 weights, so the multiplication is next to free up to 16 tokens, and the fragments come
+// instruction per 512 bytes of bf16 weights, so the multiplication is next to free, and the fragments come
 // from shared memory without passing through tensor memory, which for tiles this thin would cost more than it gives (tcgen05's
 // smallest tile has 64 rows: more than a CTA's share of the rows of small layers).  fp32 rows take plain FMAs, a lane per row.
 #pragma once
@@ -50,42 +50,53 @@ template <> struct RsFormat<__nv_bfloat16> {
   typedef __nv_bfloat16 X;                       // the tokens' type
   static constexpr int COLS = 64;                // columns of a chunk
   static constexpr int ROW = 128, XROW = 128;    // their bytes in a weight row, in a token's row
-  static constexpr int SCALES = 0, GROUP = 1, GROUPS = 1;  // bytes of scales in a stage; columns of a group, groups of a chunk
+  static constexpr int GROUP = 1, GROUPS = 0;    // (4 bits) columns of a group, groups of a chunk
 };
 template <> struct RsFormat<float> {
   typedef float X;
-  static constexpr int COLS = 32, ROW = 128, XROW = 128, SCALES = 0, GROUP = 1, GROUPS = 1;
+  static constexpr int COLS = 32, ROW = 128, XROW = 128, GROUP = 1, GROUPS = 0;
 };
 template <int G> struct RsFormat<W4<G>> {
   typedef __nv_bfloat16 X;
-  static constexpr int COLS = 128, ROW = 64, XROW = 256, GROUP = G, GROUPS = COLS / G;
-  static constexpr int SCALES = GROUPS * 2 * 9 * 4;  // per group two runs of nine words (16 scales from an odd one on)
+  static constexpr int COLS = G == 32 ? 128 : 256;  // (as many scales as 32 columns have leave no room for three longer stages)
+  static constexpr int ROW = COLS / 2, XROW = COLS * 2, GROUP = G, GROUPS = COLS / G;
 };
-template <typename W, int NT> struct RsSizes {   // NT: tokens, in eights
+template <typename W, int NT> struct RsSizes {   // NT: token slots, in eights
   typedef RsFormat<W> F;
+  static constexpr int WARPS = 8, THREADS = 32 * WARPS;
   static constexpr int A = kRsTile * F::ROW, X = 8 * NT * F::XROW;
-  static constexpr int STAGE = (A + X + F::SCALES + 15) / 16 * 16;
+  static constexpr int SCALES = F::GROUPS * 2 * 9 * 4;  // per group two runs of nine words (16 scales from an odd one on)
+  static constexpr int STAGE = (A + X + SCALES + 15) / 16 * 16;
   static constexpr int REGS = 8 * NT;            // sums per lane
-  static constexpr int WARPS = F::SCALES > 0 ? 16 : 8, THREADS = 32 * WARPS;
-  static constexpr int SLOTS = WARPS * REGS * 32 * 4;
-  static constexpr int ROOM = 219 * 1024 - SLOTS;  // (8 KB are left for the kernels' own tables)
+  static constexpr int SLOT = 16 * kRsTile;      // floats of a warp's slot: its sums of a tile, or (kRsSum) 16 tokens' sums of its rows
+  static constexpr int SLOTS = WARPS * SLOT * 4;
+  static constexpr int ROOM = 218 * 1024 - SLOTS;  // (9 KB are left for the kernels' own tables)
   static constexpr int STAGES = ROOM / (WARPS * STAGE) < 6 ? ROOM / (WARPS * STAGE) : 6;
   static constexpr int RING = WARPS * STAGES * STAGE;
   static constexpr int BYTES = RING + SLOTS;     // dynamic shared memory
+  static_assert(STAGES >= 2 && REGS * 32 <= SLOT, "a stage to fill beside one to read; a tile's sums fit a slot");
 };
 
-// A product's matrix and tokens.  Tokens of matrix number u (a matrix that some token needs) are rows x + u * x_step + t * C.
+// A product's matrices and tokens.
 struct RsOperand {
   const void* w0;               // rows of run 0: [matrices, N, C]
   const void* w1;               // rows of run 1 (gate / up: the other matrix's; else w0)
   const __nv_bfloat16* s0;      // 4 bits: scales [matrices, C / group, N]
   const __nv_bfloat16* s1;
-  const void* x;
-  long long x_step;             // elements
+  const void* x;                // token rows [.., C]
   int N, C, matrices;           // matrices: all there are
 };
 
-// The rows of one CTA: [begin, end) of `used` matrices' rows laid end to end.  RT: rows of a tile.
+// What is to be multiplied: entries, each a matrix and the up to 8 * NT tokens that it is for (a matrix with more tokens has
+// several entries, which share its reading in L2).  In shared memory.
+struct RsList {
+  const unsigned short* used;   // matrix of an entry
+  const unsigned char* count;   // its tokens
+  const unsigned char* token;   // [8 * NT] per entry: the rows of x (kRsSum: row entry * 8 * NT + slot, and this names the outputs)
+  int n;
+};
+
+// The rows of one CTA: [begin, end) of `used` entries' rows laid end to end.  RT: rows of a tile.
 struct RsRange {
   long long begin, end;
   int N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
@@ -122,30 +133,23 @@ struct RsRange {
 };
 
 enum RsKind {
-  kRsPairs,   // tiles of up to 16 pairs: row f of w0 and row f of w1, of one matrix each
-  kRsRows,    // tiles of up to 32 rows of one matrix each
-  kRsSum,     // tiles of up to 32 rows, the same rows of every used matrix one after the other, weighted and added
+  kRsPairs,   // tiles of up to 16 pairs: row f of w0 and row f of w1, of one entry each
+  kRsRows,    // tiles of up to 32 rows of one entry each
+  kRsSum,     // tiles of up to 32 rows, the same rows of every entry one after the other, weighted and added per token
 };
 
-// Which matrices, and which tokens each is for; read from shared memory.
-struct RsList {
-  const int* used;              // matrix of each number
-  const unsigned short* mask;   // tokens of each number
-  int n;
-};
-
-// A warp's way through its units.  KIND as above.
+// A warp's way through its units.
 template <typename W, int NT, int KIND>
 struct RowStream {
   typedef RsFormat<W> F;
   typedef RsSizes<W, NT> Z;
   typedef typename F::X X;
-  static constexpr int REGS = Z::REGS, WARPS = Z::WARPS;
+  static constexpr int REGS = Z::REGS, WARPS = Z::WARPS, SLOTS = 8 * NT;
   static constexpr bool kMma = sizeof(X) == 2;
-  static constexpr bool k4Bit = F::SCALES > 0;
+  static constexpr bool k4Bit = F::GROUPS > 0;
   static constexpr int LPR = F::ROW / 16;         // lanes per weight row of a copy instruction
   static constexpr int RPI = 32 / LPR;            // rows per instruction
-  static constexpr int XLPR = F::XROW / 16, XRPI = 32 / XLPR;
+  static constexpr int XLPR = F::XROW / 16, XRPI = 32 / XLPR, XI = SLOTS / XRPI;
 
   const RsOperand& op;
   const RsList& list;
@@ -154,9 +158,10 @@ struct RowStream {
   long long unit, unit_end;  // what is left to copy, as unit numbers
   // where the copies are
   int tile_i, chunk, u, row, n0, n1;  // chunk: of the matrix
-  const char *pa0, *pa1, *px;  // the lane's first bytes of the unit
-  long long scale_at;          // (4 bits) the lane's run's first scale of the unit's first group
-  unsigned mask;
+  const char *pa0, *pa1;     // the lane's first bytes of the unit
+  long long scale_at;        // (4 bits) the lane's run's first scale of the unit's first group
+  uint32_t px[XI];           // the lane's first byte of each of its tokens
+  int count;                 // tokens, less the lane's first slot
   uint32_t ring;             // shared address of the warp's ring
   int lane;
 
@@ -194,8 +199,12 @@ struct RowStream {
     const long long at = (long long)(lane / LPR) * ld + (long long)chunk * F::ROW + lane % LPR * 16;
     pa0 = (const char*)op.w0 + (e * op.N + row) * ld + at;
     pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
-    px = (const char*)op.x + ((long long)u * op.x_step + (long long)(lane / XLPR) * op.C) * (int)sizeof(X) + (long long)chunk * F::XROW + lane % XLPR * 16;
-    mask = list.mask[u];
+    count = (int)list.count[u] - lane / XLPR;
+#pragma unroll
+    for (int i = 0; i < XI; ++i) {
+      const int slot = u * SLOTS + i * XRPI + lane / XLPR;
+      px[i] = (uint32_t)(KIND == kRsSum ? slot : (int)list.token[slot]) * (uint32_t)(op.C * (int)sizeof(X)) + (uint32_t)chunk * F::XROW + lane % XLPR * 16;
+    }
     if constexpr (k4Bit) scale_at = (e * (op.C / F::GROUP) + (long long)chunk * F::GROUPS) * op.N + (lane < 16 ? row : row1(row, n0));
   }
 
@@ -203,7 +212,8 @@ struct RowStream {
     ++unit;
     pa0 += F::ROW;
     pa1 += F::ROW;
-    px += F::XROW;
+#pragma unroll
+    for (int i = 0; i < XI; ++i) px[i] += F::XROW;
     if constexpr (k4Bit) scale_at += (long long)F::GROUPS * op.N;
     if (++chunk == chunks && unit < unit_end) {
       chunk = 0;
@@ -218,8 +228,7 @@ struct RowStream {
   }
 
   // The weights (and scales) of the current unit into a stage.
-  __device__ __forceinline__ void copy_weights(int stage) const {
-    const uint32_t dst = ring + stage * Z::STAGE;
+  __device__ __forceinline__ void copy_weights(uint32_t dst) const {
     const long long step = RPI * row_bytes();
     const bool some = chunk * F::ROW + lane % LPR * 16 < (int)row_bytes();
     const char *a0 = some ? pa0 : (const char*)op.w0, *a1 = some ? pa1 : (const char*)op.w1;  // (zeros beyond the row)
@@ -238,6 +247,7 @@ struct RowStream {
   }
   // Shared-memory placement of 16-byte unit c of row r, so that eight rows' same unit lie in different banks.
   __device__ __forceinline__ static int row_unit(int r, int c) { return F::ROW == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
+  // Of a token's: read by rows of eight (bf16), one row at a time (fp32), or two rows of four units at a time (4 bits).
   __device__ __forceinline__ static int token_unit(int t, int c) { return F::XROW == 128 ? c ^ (t & 7) : c ^ ((t & 1) << 2); }
 
   // Scale words: [group of the chunk][run][9], 16 rows from an even element on; half a warp per run.
@@ -258,31 +268,28 @@ struct RowStream {
   }
 
   // The tokens' columns of the current unit.
-  __device__ __forceinline__ void copy_tokens(int stage) const {
-    const uint32_t dst = ring + stage * Z::STAGE + Z::A;
+  __device__ __forceinline__ void copy_tokens(uint32_t dst) const {
     const bool some = chunk * F::XROW + lane % XLPR * 16 < op.C * (int)sizeof(X);
-    const long long step = some ? XRPI * (long long)op.C * (int)sizeof(X) : 0;
-    const char* x = some ? px : (const char*)op.x;
-    const unsigned mine = mask >> (lane / XLPR);
 #pragma unroll
-    for (int i = 0; i < 8 * NT / XRPI; ++i) {
+    for (int i = 0; i < XI; ++i) {
       const int t = i * XRPI + lane / XLPR;
-      if ((mine >> (i * XRPI)) & 1u) copy16(dst + t * F::XROW + token_unit(t, lane % XLPR) * 16, x, some);
-      x += step;
+      if (i * XRPI < count)
+        copy16(dst + Z::A + t * F::XROW + token_unit(t, lane % XLPR) * 16, (const char*)op.x + (some ? px[i] : 0u), some);
     }
   }
 
-  // One stage's products added to acc.  two: the runs have more than 8 rows.  odd0, odd1: bit q, whether the runs' scales of group q
-  // begin in the second half of their first word.
-  __device__ __forceinline__ void multiply(int stage, unsigned mask, bool two, unsigned odd0, unsigned odd1, float (&acc)[REGS]) const {
-    const uint32_t a = ring + stage * Z::STAGE, x = a + Z::A;
+  // One stage's products added to acc.  MT: 1 where the runs have at most 8 rows, else 2.  odd0, odd1: bit q, whether the runs'
+  // scales of group q begin in the second half of their first word.  (Slots without a token hold anything: their sums are not read.)
+  template <int MT>
+  __device__ __forceinline__ void multiply(uint32_t a, int tokens, unsigned odd0, unsigned odd1, float (&acc)[REGS]) const {
+    const uint32_t x = a + Z::A;
     if constexpr (!kMma) {
       float w[32];
 #pragma unroll
       for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + lane * F::ROW + row_unit(lane, c) * 16), w + 4 * c);
 #pragma unroll
-      for (int t = 0; t < 8 * NT; ++t) {
-        if (!((mask >> t) & 1u)) continue;
+      for (int t = 0; t < SLOTS; ++t) {
+        if (t >= tokens) break;
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
@@ -298,38 +305,33 @@ struct RowStream {
     } else if constexpr (!k4Bit) {
       uint32_t b[NT][4][2];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        if (!((mask >> (8 * t)) & 0xffu)) continue;
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t r[4];
           ldsm4(x + (8 * t + lane % 8) * F::XROW + token_unit(lane % 8, 4 * q + lane / 8) * 16, r);
           b[t][2 * q][0] = r[0]; b[t][2 * q][1] = r[1]; b[t][2 * q + 1][0] = r[2]; b[t][2 * q + 1][1] = r[3];
         }
-      }
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        if (m == 1 && !two) break;
-        const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int m = 0; m < MT; ++m) {
+          const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
           uint32_t w[4];
           ldsm4(a + r * F::ROW + row_unit(r, 2 * k + lane / 16) * 16, w);
 #pragma unroll
           for (int t = 0; t < NT; ++t)
-            if ((mask >> (8 * t)) & 0xffu) mma16816(reinterpret_cast<float(&)[4]>(acc[(m * NT + t) * 4]), w[0], w[1], w[2], w[3], b[t][k][0], b[t][k][1]);
+            mma16816(reinterpret_cast<float(&)[4]>(acc[(m * NT + t) * 4]), w[0], w[1], w[2], w[3], b[t][k][0], b[t][k][1]);
         }
-      }
     } else {
       const uint32_t sc = x + Z::X;
       constexpr int per_group = F::GROUP / 32;  // 32-column units
-      float part[2][NT][4];
+      float part[MT][NT][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {         // 64 columns each
-        uint32_t w[2][4];
+      for (int h = 0; h < F::COLS / 64; ++h) {  // 64 columns each
+        uint32_t w[MT][4];
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          if (m == 1 && !two) break;
+        for (int m = 0; m < MT; ++m) {
           const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
           ldsm4(a + r * F::ROW + row_unit(r, 2 * h + lane / 16) * 16, w[m]);
         }
@@ -338,30 +340,26 @@ struct RowStream {
           const int k = 2 * h + v;          // 32-column unit
           if (k % per_group == 0) {
 #pragma unroll
-            for (int j = 0; j < 8 * NT; ++j) part[j / (4 * NT)][j / 4 % NT][j % 4] = 0.0f;
+            for (int j = 0; j < 4 * MT * NT; ++j) part[j / (4 * NT)][j / 4 % NT][j % 4] = 0.0f;
           }
           uint4 b[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            if ((mask >> (8 * t)) & 0xffu) b[t] = lds128(x + (8 * t + lane / 4) * F::XROW + token_unit(lane / 4, 4 * k + lane % 4) * 16);
+          for (int t = 0; t < NT; ++t) b[t] = lds128(x + (8 * t + lane / 4) * F::XROW + token_unit(lane / 4, 4 * k + lane % 4) * 16);
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            if (m == 1 && !two) break;
+          for (int m = 0; m < MT; ++m) {
             uint32_t d0[4], d1[4];
             dequantise(w[m][2 * v], d0);
             dequantise(w[m][2 * v + 1], d1);
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              if ((mask >> (8 * t)) & 0xffu) {
-                mma16816(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t].x, b[t].y);
-                mma16816(part[m][t], d0[2], d1[2], d0[3], d1[3], b[t].z, b[t].w);
-              }
+            for (int t = 0; t < NT; ++t) {
+              mma16816(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t].x, b[t].y);
+              mma16816(part[m][t], d0[2], d1[2], d0[3], d1[3], b[t].z, b[t].w);
+            }
           }
           if ((k + 1) % per_group == 0) {   // the group's sums, scaled once
             const int q = k / per_group;
 #pragma unroll
-            for (int m = 0; m < 2; ++m) {
-              if (m == 1 && !two) break;
+            for (int m = 0; m < MT; ++m) {
               const float f0 = scale(sc, 2 * q, 8 * m + lane / 4 + ((odd0 >> q) & 1));
               const float f1 = scale(sc, 2 * q + 1, 8 * m + lane / 4 + ((odd1 >> q) & 1));
 #pragma unroll
@@ -394,32 +392,36 @@ struct RowStream {
     asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(sc + pair * 36 + i * 2) : "memory");
     return __uint_as_float((uint32_t)v << 16);
   }
+
   // ---- the warp's loop: prefetch() [the weights alone, before the tokens exist], run(), then a barrier of the CTA, then join() ----
 
   // Where the products are; what run() leaves of a tile that goes on in the next warps' shares.
-  int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_base;
-  unsigned m_mask;
+  int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_base, m_tokens;
   bool pending;
-  float sum[REGS];
+  float acc[REGS];
 
   __device__ __forceinline__ void prefetch() {
     __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < Z::STAGES - 1; ++i)
       if (unit < unit_end) {
-        copy_weights(i);
+        copy_weights(ring + i * Z::STAGE);
         advance();
       }
     copies_commit();
   }
 
   __device__ __forceinline__ void set_matrix() {
-    m_mask = list.mask[m_u];
+    m_tokens = list.count[m_u];
     if constexpr (k4Bit) m_base = list.used[m_u] * (op.C / F::GROUP);
   }
+  // kRsSum: where a warp adds up its rows' results per token.  (The rows are swizzled so that the lanes of a fragment, which
+  // hold eight rows of four tokens, hit different banks.)
+  __device__ __forceinline__ static int sum_at(int t, int r) { return t * kRsTile + (r ^ ((t & 3) << 3)); }
 
-  // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, t): of a token for a matrix
-  // (kRsSum).  finish(u, row, n0, n1, sums): a whole tile.  slots: shared memory for cut tiles, Z::SLOTS bytes.
+  // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, slot): of a token for an entry
+  // (kRsSum).  finish(u, row, n0, n1, sums): a whole tile, whose sums are in acc or (kRsSum) in shared memory at sum_at().
+  // slots: shared memory, Z::SLOTS bytes.
   template <typename Weight, typename Finish>
   __device__ __forceinline__ void run(RowStream* start, float* slots, Weight weight, Finish finish) {
     const RowStream& at = start != nullptr ? *start : *this;
@@ -431,25 +433,29 @@ struct RowStream {
       return;
     }
     set_matrix();
+    float* slot = slots + threadIdx.x / 32 * Z::SLOT;
     bool cut = KIND == kRsSum ? m_u != 0 || m_chunk != 0 : m_chunk != 0;  // the tile begins in an earlier warp's share
+    float held[Z::SLOT / 32];
+    bool hold = false;
 #pragma unroll 1
     for (int i = 0; i < Z::STAGES - 1; ++i) {
       if (i < total) {
         if (start != nullptr) {
-          start->copy_tokens(i);
+          start->copy_tokens(ring + i * Z::STAGE);
           start->advance();
         } else {
-          copy_weights(i);
-          copy_tokens(i);
+          copy_weights(ring + i * Z::STAGE);
+          copy_tokens(ring + i * Z::STAGE);
           advance();
         }
       }
       copies_commit();
     }
-    float acc[REGS];
 #pragma unroll
-    for (int j = 0; j < REGS; ++j) acc[j] = sum[j] = 0.0f;
-    int stage = 0, next = Z::STAGES - 1;
+    for (int j = 0; j < REGS; ++j) acc[j] = 0.0f;
+    if (KIND == kRsSum)
+      for (int j = lane; j < Z::SLOT; j += 32) slot[j] = 0.0f;
+    uint32_t stage = ring, next = ring + (Z::STAGES - 1) * Z::STAGE;
 #pragma unroll 1
     for (int i = 0; i < total; ++i) {
       __syncwarp();
@@ -463,13 +469,14 @@ struct RowStream {
       __syncwarp();
       unsigned odd0 = 0, odd1 = 0;
       if constexpr (k4Bit) {  // scale number (matrix's + group) * N + row
-        const unsigned swing = op.N & 1 ? 0xau ^ ((m_base + m_chunk * F::GROUPS) & 1 ? 0xfu : 0u) : 0u;
-        odd0 = swing ^ (m_row & 1 ? 0xfu : 0u);
-        odd1 = swing ^ (row1(m_row, m_n0) & 1 ? 0xfu : 0u);
+        const unsigned swing = op.N & 1 ? 0xaau ^ ((m_base + m_chunk * F::GROUPS) & 1 ? 0xffu : 0u) : 0u;
+        odd0 = swing ^ (m_row & 1 ? 0xffu : 0u);
+        odd1 = swing ^ (row1(m_row, m_n0) & 1 ? 0xffu : 0u);
       }
-      multiply(stage, m_mask, m_n0 > 8, odd0, odd1, acc);
+      if (m_n0 > 8) multiply<2>(stage, m_tokens, odd0, odd1, acc);
+      else multiply<1>(stage, m_tokens, odd0, odd1, acc);
       next = stage;
-      stage = stage + 1 == Z::STAGES ? 0 : stage + 1;
+      stage = stage + Z::STAGE == ring + Z::STAGES * Z::STAGE ? ring : stage + Z::STAGE;
       ++m_chunk;
       const bool last = i + 1 == total;
       if (m_chunk < chunks && !last) continue;
@@ -478,29 +485,31 @@ struct RowStream {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
           const int t = token(j);
-          if ((m_mask >> t) & 1u) sum[j] = __fmaf_rn(weight(m_u, t), acc[j], sum[j]);  // (the other tokens' sums hold anything)
+          if (t < m_tokens) {
+            float* to = slot + sum_at(list.token[m_u * SLOTS + t], run_of(j) * kRsRun + row_of(j));
+            *to = __fmaf_rn(weight(m_u, t), acc[j], *to);
+          }
           acc[j] = 0.0f;
         }
+        __syncwarp();
         if (m_chunk == chunks && m_u + 1 < list.n) {
           ++m_u;
           m_chunk = 0;
           set_matrix();
           if (!last) continue;
         }
-      } else {
-#pragma unroll
-        for (int j = 0; j < REGS; ++j) {
-          sum[j] = acc[j];
-          acc[j] = 0.0f;
-        }
       }
-      const bool whole = m_chunk == chunks;  // (kRsSum: of the last matrix)
       if (cut) {
-        float* slot = slots + (threadIdx.x / 32) * (REGS * 32) + lane;
+        if (KIND == kRsSum) {
 #pragma unroll
-        for (int j = 0; j < REGS; ++j) slot[j * 32] = sum[j];
-      } else if (whole) {
-        finish(m_u, m_row, m_n0, m_n1, sum);
+          for (int j = 0; j < Z::SLOT / 32; ++j) held[j] = slot[j * 32 + lane];
+          hold = true;
+        } else {
+#pragma unroll
+          for (int j = 0; j < REGS; ++j) slot[j * 32 + lane] = acc[j];
+        }
+      } else if (m_chunk == chunks) {  // (kRsSum: of the last entry)
+        finish(m_u, m_row, m_n0, m_n1, slot);
       } else {
         pending = true;
       }
@@ -510,32 +519,52 @@ struct RowStream {
         set_tile(++m_tile, m_u, m_row, m_n0, m_n1);
         if (KIND == kRsSum) {
           m_u = 0;
-#pragma unroll
-          for (int j = 0; j < REGS; ++j) sum[j] = 0.0f;
+          __syncwarp();
+          for (int j = lane; j < Z::SLOT; j += 32) slot[j] = 0.0f;
+          __syncwarp();
         }
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) acc[j] = 0.0f;
         set_matrix();
       }
     }
     copies_wait<0>();
+    if (KIND == kRsSum && hold) {  // the ring is free now
+      __syncwarp();
+      float* area = held_area(threadIdx.x / 32);
+#pragma unroll
+      for (int j = 0; j < Z::SLOT / 32; ++j) area[j * 32 + lane] = held[j];
+    }
   }
 
   // Behind the barrier: the warp that a cut tile begins in adds what the following warps left, and finishes it.
   template <typename Finish>
-  __device__ __forceinline__ void join(const float* slots, Finish finish) {
+  __device__ __forceinline__ void join(float* slots, Finish finish) {
     if (!pending) return;
     const long long units = (long long)range.tiles * per_tile, tile_end = (long long)(m_tile + 1) * per_tile;
+    float* slot = slots + threadIdx.x / 32 * Z::SLOT;
     for (int w = threadIdx.x / 32 + 1; w < WARPS; ++w) {
       const long long begin = units * w / WARPS;
       if (begin >= tile_end) break;
       if (units * (w + 1) / WARPS == begin) continue;
-      const float* slot = slots + w * (REGS * 32) + lane;
+      if (KIND == kRsSum) {
+        const float* area = held_area(w);
 #pragma unroll
-      for (int j = 0; j < REGS; ++j) sum[j] += slot[j * 32];
+        for (int j = 0; j < Z::SLOT / 32; ++j) slot[j * 32 + lane] += area[j * 32 + lane];
+      } else {
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) acc[j] += slots[w * Z::SLOT + j * 32 + lane];
+      }
     }
-    finish(m_u, m_row, m_n0, m_n1, sum);
+    __syncwarp();
+    finish(m_u, m_row, m_n0, m_n1, slot);
+  }
+  // kRsSum: warp w's sums of a tile that began before its share, in its ring.
+  __device__ __forceinline__ float* held_area(int w) const {
+    return reinterpret_cast<float*>(__cvta_shared_to_generic(ring + (w - (int)threadIdx.x / 32) * (Z::STAGES * Z::STAGE)));
   }
 
-  // Of sum number j: the token, and (tensor cores) the run, the row in it.
+  // Of sum number j: the token's slot, the run, the row in it.
   __device__ __forceinline__ int token(int j) const { return kMma ? j / 4 % NT * 8 + lane % 4 * 2 + j % 2 : j; }
   __device__ __forceinline__ int run_of(int j) const { return kMma ? j / 2 % 2 : lane / kRsRun; }
   __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun; }

@@ -120,8 +120,6 @@ static cudaError_t launch_unpack(const moe_w4_t& w, size_t words, int N, int C, 
 
 // ---- products with a few rows ------------------------------------------------------------------------------------------------
 
-constexpr int kMatvecRows = MOE_FEW_MAX_TOKENS;  // at a time
-
 struct W4MatvecParams {
   const void* codes;
   const __nv_bfloat16* scales;
@@ -131,44 +129,51 @@ struct W4MatvecParams {
   int experts, N, C, M;
 };
 
-// Rows of x are taken sixteen (NT 1: eight) at a time; those with the same matrix share its reading.
+// Rows of x are taken `batch` at a time: 8 * NT of one matrix, or 32 of several; rows with the same matrix share its
+// reading by eights.
 template <int G, int NT>
 __global__ void __launch_bounds__(RsSizes<W4<G>, NT>::THREADS, 1)
-w4_matvec_kernel(const __grid_constant__ W4MatvecParams p) {
+w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
   typedef RsSizes<W4<G>, NT> Z;
+  constexpr int SLOTS = 8 * NT;
   extern __shared__ __align__(128) unsigned char dynamic[];
-  __shared__ int used[kMatvecRows], n_used;
-  __shared__ unsigned short mask[kMatvecRows];
+  __shared__ unsigned short used[32];
+  __shared__ unsigned char count[32], token[32 * SLOTS];
+  __shared__ int entries;
   float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
   const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
   const int lane = threadIdx.x % 32;
-  for (int m0 = 0; m0 < p.M; m0 += 8 * NT) {
-    const int rows = min(8 * NT, p.M - m0);
-    if (threadIdx.x < 32) {  // the matrices in the order of the first row that wants them
+  for (int m0 = 0; m0 < p.M; m0 += batch) {
+    const int rows = min(batch, p.M - m0);
+    if (threadIdx.x < 32) {  // an entry per matrix and SLOTS rows of it, in the order of their first rows
       int e = lane < rows ? p.expert != nullptr ? p.expert[m0 + lane] : 0 : -1;
       if (e < 0 || e >= p.experts) e = -1;
       const unsigned same = __match_any_sync(0xffffffffu, e);
-      const bool first = e >= 0 && lane == __ffs(same) - 1;
+      const int rank = __popc(same & ((1u << lane) - 1u));
+      const bool first = e >= 0 && rank % SLOTS == 0;
       const unsigned firsts = __ballot_sync(0xffffffffu, first);
+      const int mine = __popc(firsts & ((1u << lane) - 1u));
+      const unsigned before = same & firsts & (0xffffffffu >> (31 - lane));  // the last of them begins this row's entry
+      const int entry = __shfl_sync(0xffffffffu, mine, before != 0 ? 31 - __clz(before) : lane);
       if (first) {
-        const int at = __popc(firsts & ((1u << lane) - 1u));
-        used[at] = e;
-        mask[at] = (unsigned short)same;
+        used[entry] = (unsigned short)e;
+        count[entry] = (unsigned char)min(SLOTS, __popc(same) - rank);
       }
-      if (lane == 0) n_used = __popc(firsts);
+      if (e >= 0) token[entry * SLOTS + rank % SLOTS] = (unsigned char)lane;
+      if (lane == 0) entries = __popc(firsts);
     }
     __syncthreads();
-    const RsList list{used, mask, n_used};
-    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts};
+    const RsList list{used, count, token, entries};
+    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, p.N, p.C, p.experts};
     typedef RowStream<W4<G>, NT, kRsRows> Stream;
     Stream rs(op, list, ring);
-    auto finish = [&](int u, int row, int n0, int n1, const float (&sum)[Z::REGS]) {
+    auto finish = [&](int u, int row, int n0, int n1, const float*) {
 #pragma unroll
       for (int j = 0; j < Z::REGS; ++j) {
         const int t = rs.token(j), r = rs.row_of(j);
         const bool second = rs.run_of(j) == 1;
-        if (((mask[u] >> t) & 1u) && r < (second ? n1 : n0))
-          p.y[(size_t)(m0 + t) * p.N + row + (second ? n0 : 0) + r] = __float2bfloat16_rn(sum[j]);
+        if (t < count[u] && r < (second ? n1 : n0))
+          p.y[(size_t)(m0 + token[u * SLOTS + t]) * p.N + row + (second ? n0 : 0) + r] = __float2bfloat16_rn(rs.acc[j]);
       }
     };
     rs.run(nullptr, slots, [](int, int) { return 0.0f; }, finish);
@@ -187,7 +192,7 @@ static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const int sms = sm_count_now();
   if (sms <= 0) return cudaErrorUnknown;
-  w4_matvec_kernel<G, NT><<<sms, RsSizes<W4<G>, NT>::THREADS, RsSizes<W4<G>, NT>::BYTES, st>>>(q);
+  w4_matvec_kernel<G, NT><<<sms, RsSizes<W4<G>, NT>::THREADS, RsSizes<W4<G>, NT>::BYTES, st>>>(q, q.experts > 1 ? 32 : 8 * NT);
   return cudaGetLastError();
 }
 
@@ -228,12 +233,13 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
   if (M < 0) return MOE_ERR_ARG;
   if (M == 0) return MOE_OK;
   if (!d_x || !d_y || (experts > 1 && !d_expert)) return MOE_ERR_ARG;
+  if (experts > 65535 || C > (1 << 25)) return MOE_ERR_UNSUPPORTED;  // (16-bit matrix numbers, 32-bit offsets into a batch of x)
   if (((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) & 15) || (reinterpret_cast<uintptr_t>(d_expert) & 3))
     return MOE_ERR_ALIGN;
   const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, M};
   cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e;
-  if (M <= 8) e = group == 32 ? launch_matvec<32, 1>(q, st) : group == 64 ? launch_matvec<64, 1>(q, st) : launch_matvec<128, 1>(q, st);
+  if (M <= 8 || experts > 1) e = group == 32 ? launch_matvec<32, 1>(q, st) : group == 64 ? launch_matvec<64, 1>(q, st) : launch_matvec<128, 1>(q, st);
   else e = group == 32 ? launch_matvec<32, 2>(q, st) : group == 64 ? launch_matvec<64, 2>(q, st) : launch_matvec<128, 2>(q, st);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
