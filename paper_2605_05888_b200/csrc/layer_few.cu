@@ -13,9 +13,7 @@
 
 namespace moehub {
 
-constexpr int kLfThreads = 256;
-constexpr int kLfWarps = kLfThreads / 32;
-static_assert(kMaxExperts == kLfThreads, "a thread per expert");
+constexpr int kLfMaxWarps = 16;
 constexpr int kLfTokens = MOE_FEW_MAX_TOKENS;
 constexpr int kLfPicks = 32;  // most picks per token
 
@@ -80,7 +78,7 @@ struct LfShared {
   int warp_used[kMaxExperts / 32];
 };
 struct LfSelect {  // where the rows are streamed through later
-  float red[kLfWarps][kLfTokens];
+  float red[kLfMaxWarps][kLfTokens];
   int idx[kLfTokens * kLfPicks];
   unsigned mask[kMaxExperts];
   int pos[kMaxExperts];  // a used expert's first entry
@@ -96,7 +94,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     const int e = task / p.slices, slice = task % p.slices;
     const int c0 = slice * p.slice_cols, c1 = min(p.H, c0 + p.slice_cols);
     float acc[kLfTokens] = {};
-    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += kLfThreads * N) {
+    for (int c = c0 + (int)threadIdx.x * N; c < c1; c += blockDim.x * N) {
       float w[N];
       Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)e * p.H + c), w);
 #pragma unroll
@@ -119,7 +117,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
     if ((int)threadIdx.x < p.T) {
       float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < (int)kLfWarps; ++i) sum += s.red[i][threadIdx.x];
+      for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += s.red[i][threadIdx.x];
       __stcg(p.logits + ((size_t)slice * p.T + threadIdx.x) * p.E + e, sum);
     }
     __syncthreads();
@@ -129,7 +127,7 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
 // Every CTA selects for itself; returns the number of entries.
 __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  for (int i = tid; i < p.T * p.E; i += kLfThreads) {
+  for (int i = tid; i < p.T * p.E; i += blockDim.x) {
     float sum = 0.0f;
     for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
     q.logits[i] = p.bias != nullptr ? sum + p.bias[i % p.E] : sum;
@@ -139,7 +137,7 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
   if (p.E <= 64) select_topk<32, 2>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   else select_topk<32, 8>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
+  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
     atomicOr(&q.mask[q.idx[a]], 1u << (a / p.K));
     if (blockIdx.x == 0)
       for (int sh = 0; sh < p.tp; ++sh) {
@@ -149,16 +147,16 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
   }
   __syncthreads();
   if (blockIdx.x == 0)
-    for (int e = tid; e < p.E * p.tp; e += kLfThreads) p.expert_count[e] = __popc(q.mask[e / p.tp]);
+    for (int e = tid; e < p.E * p.tp; e += blockDim.x) p.expert_count[e] = __popc(q.mask[e / p.tp]);
   // entries: one per used expert and eight tokens of it
-  const int tokens = __popc(q.mask[tid]), entries = (tokens + kLfSlots - 1) / kLfSlots;
+  const int tokens = tid < kMaxExperts ? __popc(q.mask[tid]) : 0, entries = (tokens + kLfSlots - 1) / kLfSlots;
   int upto = entries;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
     const int v = __shfl_up_sync(0xffffffffu, upto, off);
     if (lane >= off) upto += v;
   }
-  if (lane == 31) s.warp_used[warp] = upto;
+  if (lane == 31 && tid < kMaxExperts) s.warp_used[warp] = upto;
   __syncthreads();
   int pos = upto - entries, n = 0;
 #pragma unroll
@@ -166,13 +164,13 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
     if (i < warp) pos += s.warp_used[i];
     n += s.warp_used[i];
   }
-  q.pos[tid] = pos;
+  if (tid < kMaxExperts) q.pos[tid] = pos;
   for (int i = 0; i < entries; ++i) {
     s.used[pos + i] = (unsigned short)tid;
     s.count[pos + i] = (unsigned char)min(kLfSlots, tokens - i * kLfSlots);
   }
   __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += kLfThreads) {
+  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
     const int t = a / p.K, e = q.idx[a], slot = q.pos[e] * kLfSlots + __popc(q.mask[e] & ((1u << t) - 1u));
     s.token[slot] = (unsigned char)t;
     s.pick[slot] = (unsigned char)(a % p.K);
@@ -184,13 +182,13 @@ __device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, L
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
 template <typename W>
-__global__ void __launch_bounds__(kLfThreads, 1)
+__global__ void __launch_bounds__(RsSizes<W, 1>::THREADS, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   typedef typename RsFormat<W>::X X;
   typedef RsSizes<W, 1> Z;
   extern __shared__ __align__(128) unsigned char dynamic[];
   __shared__ LfShared s;
-  static_assert(sizeof(LfSelect) <= Z::RING && Z::THREADS == kLfThreads, "the selection's tables lie in the ring");
+  static_assert(sizeof(LfSelect) <= Z::RING && Z::WARPS <= kLfMaxWarps && Z::THREADS >= kMaxExperts, "the selection's tables lie in the ring");
   LfSelect& q = *reinterpret_cast<LfSelect*>(dynamic);
   float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
   const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
@@ -243,7 +241,7 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p->sm_count);
-  cfg.blockDim = dim3(kLfThreads);
+  cfg.blockDim = dim3(RsSizes<W, 1>::THREADS);
   cfg.dynamicSmemBytes = RsSizes<W, 1>::BYTES;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];

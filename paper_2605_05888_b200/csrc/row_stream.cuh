@@ -3,7 +3,7 @@
 // A CTA has a range of matrix rows, cut into tiles of up to 32, and every tile into chunks of columns; its warps take equal,
 // contiguous shares of all (tile, chunk) units, so that they have the same number of bytes to read whatever the sizes are.  Each warp
 // copies its own units into its own ring of shared memory (16-byte asynchronous copies: bytes in flight without registers,
-// no barrier between warps) and multiplies them by the tokens' columns, which come along in the same stage.
+// no barrier between warps) and multiplies them by the tokens' columns: these come along in the stage, or (4 bits) straight into registers where they are needed.
 // A tile that lies in one warp's share is finished from registers; of a tile that is cut, the warps after the first leave their
 // sums in shared memory and the first adds them up, in order, so the sum does not depend on timing.
 //
@@ -19,10 +19,11 @@ namespace moehub {
 
 constexpr int kRsTile = 32;   // rows of a tile: two runs of up to 16 consecutive rows
 constexpr int kRsRun = 16;
+constexpr int kRsRowBytes = 128;  // of a chunk
 
-// 16 bytes (or zeros) into shared memory, past L1
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool some) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
+// 16 bytes into shared memory, past L1 (bytes 16), or zeros (bytes 0: nothing is read)
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -37,10 +38,9 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
 }
 
 // ---- the weights' formats ----------------------------------------------------------------------------------------------------
@@ -48,25 +48,26 @@ template <int GROUP> struct W4 {};  // (4 bits; float and __nv_bfloat16 name the
 template <typename W> struct RsFormat;
 template <> struct RsFormat<__nv_bfloat16> {
   typedef __nv_bfloat16 X;                       // the tokens' type
-  static constexpr int COLS = 64;                // columns of a chunk
-  static constexpr int ROW = 128, XROW = 128;    // their bytes in a weight row, in a token's row
+  static constexpr int COLS = 64;                // columns of a chunk: 128 bytes of a row
   static constexpr int GROUP = 1, GROUPS = 0;    // (4 bits) columns of a group, groups of a chunk
+  static constexpr int WARPS = 8;
 };
 template <> struct RsFormat<float> {
   typedef float X;
-  static constexpr int COLS = 32, ROW = 128, XROW = 128, GROUP = 1, GROUPS = 0;
+  static constexpr int COLS = 32, GROUP = 1, GROUPS = 0, WARPS = 8;
 };
 template <int G> struct RsFormat<W4<G>> {
   typedef __nv_bfloat16 X;
-  static constexpr int COLS = G == 32 ? 128 : 256;  // (as many scales as 32 columns have leave no room for three longer stages)
-  static constexpr int ROW = COLS / 2, XROW = COLS * 2, GROUP = G, GROUPS = COLS / G;
+  static constexpr int COLS = 256, GROUP = G, GROUPS = COLS / G;
+  static constexpr int WARPS = 16;               // (bound by the instructions that unpack the codes)
 };
 template <typename W, int NT> struct RsSizes {   // NT: token slots, in eights
   typedef RsFormat<W> F;
-  static constexpr int WARPS = 8, THREADS = 32 * WARPS;
-  static constexpr int A = kRsTile * F::ROW, X = 8 * NT * F::XROW;
+  static constexpr int WARPS = NT == 1 ? F::WARPS : 8, THREADS = 32 * WARPS;
+  static constexpr int A = kRsTile * kRsRowBytes;
+  static constexpr int X = F::GROUPS == 0 ? 8 * NT * kRsRowBytes : 0;
   static constexpr int SCALES = F::GROUPS * 2 * 9 * 4;  // per group two runs of nine words (16 scales from an odd one on)
-  static constexpr int STAGE = (A + X + SCALES + 15) / 16 * 16;
+  static constexpr int STAGE = (A + X + SCALES + 127) / 128 * 128;
   static constexpr int REGS = 8 * NT;            // sums per lane
   static constexpr int SLOT = 16 * kRsTile;      // floats of a warp's slot: its sums of a tile, or (kRsSum) 16 tokens' sums of its rows
   static constexpr int SLOTS = WARPS * SLOT * 4;
@@ -74,7 +75,7 @@ template <typename W, int NT> struct RsSizes {   // NT: token slots, in eights
   static constexpr int STAGES = ROOM / (WARPS * STAGE) < 6 ? ROOM / (WARPS * STAGE) : 6;
   static constexpr int RING = WARPS * STAGES * STAGE;
   static constexpr int BYTES = RING + SLOTS;     // dynamic shared memory
-  static_assert(STAGES >= 2 && REGS * 32 <= SLOT, "a stage to fill beside one to read; a tile's sums fit a slot");
+  static_assert(STAGES >= 2 && REGS * 32 <= SLOT && STAGES * STAGE >= SLOT * 4, "a stage to fill beside one to read; a tile's sums fit a slot, a slot the ring");
 };
 
 // A product's matrices and tokens.
@@ -147,21 +148,20 @@ struct RowStream {
   static constexpr int REGS = Z::REGS, WARPS = Z::WARPS, SLOTS = 8 * NT;
   static constexpr bool kMma = sizeof(X) == 2;
   static constexpr bool k4Bit = F::GROUPS > 0;
-  static constexpr int LPR = F::ROW / 16;         // lanes per weight row of a copy instruction
-  static constexpr int RPI = 32 / LPR;            // rows per instruction
-  static constexpr int XLPR = F::XROW / 16, XRPI = 32 / XLPR, XI = SLOTS / XRPI;
+  static constexpr int RPI = 4;                   // rows of a copy instruction: eight lanes each
+  static constexpr int HALF = 128;                // (4 bits) columns whose tokens are in registers: half a chunk
 
   const RsOperand& op;
   const RsList& list;
   RsRange range;
   int chunks, per_tile;      // chunks of a matrix row, of a tile
-  long long unit, unit_end;  // what is left to copy, as unit numbers
+  int total, left;           // units of the share; how many are still to be copied
   // where the copies are
   int tile_i, chunk, u, row, n0, n1;  // chunk: of the matrix
   const char *pa0, *pa1;     // the lane's first bytes of the unit
-  long long scale_at;        // (4 bits) the lane's run's first scale of the unit's first group
-  uint32_t px[XI];           // the lane's first byte of each of its tokens
-  int count;                 // tokens, less the lane's first slot
+  const char* ps;            // (4 bits, N even) the lane's scale word of the unit's first group
+  bool has_scale;
+  const char* px[2 * NT];    // (not 4 bits) the lane's bytes of tokens lane / 8, 4 + lane / 8, ..
   uint32_t ring;             // shared address of the warp's ring
   int lane;
 
@@ -172,9 +172,9 @@ struct RowStream {
     per_tile = KIND == kRsSum ? chunks * list.n : chunks;
     const long long units = (long long)range.tiles * per_tile;
     const int warp = threadIdx.x / 32;
-    unit = units * warp / WARPS;
-    unit_end = units * (warp + 1) / WARPS;
-    if (unit < unit_end) {
+    const long long unit = units * warp / WARPS;
+    total = left = (int)(units * (warp + 1) / WARPS - unit);
+    if (left > 0) {
       tile_i = (int)(unit / per_tile);
       const int c = (int)(unit - (long long)tile_i * per_tile);
       set_tile(tile_i, u, row, n0, n1);
@@ -196,26 +196,35 @@ struct RowStream {
   __device__ __forceinline__ long long row_bytes() const { return k4Bit ? op.C / 2 : (long long)op.C * (int)sizeof(X); }
   __device__ __forceinline__ void set_pointers() {
     const long long e = list.used[u], ld = row_bytes();
-    const long long at = (long long)(lane / LPR) * ld + (long long)chunk * F::ROW + lane % LPR * 16;
+    const long long at = (long long)(lane / 8) * ld + (long long)chunk * kRsRowBytes + lane % 8 * 16;
     pa0 = (const char*)op.w0 + (e * op.N + row) * ld + at;
     pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
-    count = (int)list.count[u] - lane / XLPR;
+    if constexpr (!k4Bit)
 #pragma unroll
-    for (int i = 0; i < XI; ++i) {
-      const int slot = u * SLOTS + i * XRPI + lane / XLPR;
-      px[i] = (uint32_t)(KIND == kRsSum ? slot : (int)list.token[slot]) * (uint32_t)(op.C * (int)sizeof(X)) + (uint32_t)chunk * F::XROW + lane % XLPR * 16;
+      for (int i = 0; i < 2 * NT; ++i)
+        px[i] = (const char*)((const X*)op.x + (long long)x_row(u, i * 4 + lane / 8) * op.C) + (long long)chunk * kRsRowBytes + lane % 8 * 16;
+    if constexpr (k4Bit) {
+      const int r = lane < 16 ? row : row1(row, n0);
+      const long long first = (e * (op.C / F::GROUP) + (long long)chunk * F::GROUPS) * op.N + r;
+      ps = (const char*)((lane < 16 ? op.s0 : op.s1) + (first & ~1ll) + 2 * (lane % 16));
+      has_scale = lane % 16 < 9 && 2 * (lane % 16) < (lane < 16 ? n0 : n1) + (r & 1);
     }
-    if constexpr (k4Bit) scale_at = (e * (op.C / F::GROUP) + (long long)chunk * F::GROUPS) * op.N + (lane < 16 ? row : row1(row, n0));
+  }
+  // The row of x of an entry's slot (one without a token: the first's).
+  __device__ __forceinline__ int x_row(int mu, int slot) const {
+    if (slot >= list.count[mu]) slot = 0;
+    return KIND == kRsSum ? mu * SLOTS + slot : (int)list.token[mu * SLOTS + slot];
   }
 
   __device__ __forceinline__ void advance() {
-    ++unit;
-    pa0 += F::ROW;
-    pa1 += F::ROW;
+    --left;
+    pa0 += kRsRowBytes;
+    pa1 += kRsRowBytes;
+    if constexpr (!k4Bit)
 #pragma unroll
-    for (int i = 0; i < XI; ++i) px[i] += F::XROW;
-    if constexpr (k4Bit) scale_at += (long long)F::GROUPS * op.N;
-    if (++chunk == chunks && unit < unit_end) {
+      for (int i = 0; i < 2 * NT; ++i) px[i] += kRsRowBytes;
+    if constexpr (k4Bit) ps += 2ll * F::GROUPS * op.N;
+    if (++chunk == chunks && left > 0) {
       chunk = 0;
       if (KIND == kRsSum && u + 1 < list.n) {
         ++u;
@@ -227,66 +236,88 @@ struct RowStream {
     }
   }
 
-  // The weights (and scales) of the current unit into a stage.
+  // The weights (and scales) of the current unit into a stage; zeros beyond the row.
   __device__ __forceinline__ void copy_weights(uint32_t dst) const {
     const long long step = RPI * row_bytes();
-    const bool some = chunk * F::ROW + lane % LPR * 16 < (int)row_bytes();
-    const char *a0 = some ? pa0 : (const char*)op.w0, *a1 = some ? pa1 : (const char*)op.w1;  // (zeros beyond the row)
-    const long long by = some ? step : 0;
-    const int limit0 = n0 - lane / LPR, limit1 = n1 - lane / LPR;
+    const int bytes = chunk * kRsRowBytes + lane % 8 * 16 < (int)row_bytes() ? 16 : 0;
+    const char *a0 = pa0, *a1 = pa1;
+    const int limit0 = n0 - lane / 8, limit1 = n1 - lane / 8;
 #pragma unroll
     for (int i = 0; i < kRsRun / RPI; ++i) {
-      const int r = i * RPI + lane / LPR;
-      const uint32_t at = dst + r * F::ROW + row_unit(r, lane % LPR) * 16;
-      if (i * RPI < limit0) copy16(at, a0, some);
-      if (i * RPI < limit1) copy16(at + kRsRun * F::ROW, a1, some);
-      a0 += by;
-      a1 += by;
+      const int r = i * RPI + lane / 8;
+      const uint32_t at = dst + place(r, lane % 8);
+      if (i * RPI < limit0) copy16(at, a0, bytes);
+      if (i * RPI < limit1) copy16(at + kRsRun * kRsRowBytes, a1, bytes);
+      a0 += step;
+      a1 += step;
     }
-    if constexpr (k4Bit) copy_scales(dst + Z::A + Z::X);
+    if constexpr (k4Bit) copy_scales(dst + Z::A);
   }
-  // Shared-memory placement of 16-byte unit c of row r, so that eight rows' same unit lie in different banks.
-  __device__ __forceinline__ static int row_unit(int r, int c) { return F::ROW == 128 ? c ^ (r & 7) : c ^ ((r >> 1) & 3); }
-  // Of a token's: read by rows of eight (bf16), one row at a time (fp32), or two rows of four units at a time (4 bits).
-  __device__ __forceinline__ static int token_unit(int t, int c) { return F::XROW == 128 ? c ^ (t & 7) : c ^ ((t & 1) << 2); }
+  // Where 16-byte unit c of a row is, so that eight rows' same unit lie in different banks.
+  __device__ __forceinline__ static int place(int r, int c) { return r * kRsRowBytes + ((c ^ (r & 7)) * 16); }
 
   // Scale words: [group of the chunk][run][9], 16 rows from an even element on; half a warp per run.
   __device__ __forceinline__ void copy_scales(uint32_t dst) const {
-    const int G = op.C / F::GROUP, i = lane % 16, n = lane < 16 ? n0 : n1;
-    const long long total = (long long)op.matrices * G * op.N;
+    const int G = op.C / F::GROUP, i = lane % 16;
+    dst += lane / 16 * 36 + i * 4;
+    if ((op.N & 1) == 0) {  // every group's scales begin like the first's
+      const char* s = ps;
+#pragma unroll
+      for (int q = 0; q < F::GROUPS; ++q) {
+        if (has_scale) copy4(dst + q * 72, s, chunk * F::GROUPS + q < G ? 4 : 0);
+        s += 2ll * op.N;
+      }
+      return;
+    }
+    const int n = lane < 16 ? n0 : n1;
+    const long long all = (long long)op.matrices * G * op.N;
     const __nv_bfloat16* s = lane < 16 ? op.s0 : op.s1;
-    long long first = scale_at;
+    long long first = ((long long)list.used[u] * G + chunk * F::GROUPS) * op.N + (lane < 16 ? row : row1(row, n0));
 #pragma unroll
     for (int q = 0; q < F::GROUPS; ++q) {
       const long long at = (first & ~1ll) + 2 * i;
-      if (i < 9) {
-        const bool some = chunk * F::GROUPS + q < G && 2 * i < n + (int)(first & 1);
-        copy4(dst + (q * 2 + lane / 16) * 36 + i * 4, some ? s + at : s, some ? (at + 1 < total ? 4 : 2) : 0);
-      }
+      const bool some = chunk * F::GROUPS + q < G && 2 * i < n + (int)(first & 1);
+      if (i < 9) copy4(dst + q * 72, some ? s + at : s, some ? (at + 1 < all ? 4 : 2) : 0);
       first += op.N;
     }
   }
 
-  // The tokens' columns of the current unit.
+  // The tokens' columns of the current unit (4 bits: see fetch_tokens).
   __device__ __forceinline__ void copy_tokens(uint32_t dst) const {
-    const bool some = chunk * F::XROW + lane % XLPR * 16 < op.C * (int)sizeof(X);
+    if constexpr (!k4Bit) {
+      const int bytes = chunk * kRsRowBytes + lane % 8 * 16 < (int)row_bytes() ? 16 : 0, limit = (int)list.count[u] - lane / 8;
 #pragma unroll
-    for (int i = 0; i < XI; ++i) {
-      const int t = i * XRPI + lane / XLPR;
-      if (i * XRPI < count)
-        copy16(dst + Z::A + t * F::XROW + token_unit(t, lane % XLPR) * 16, (const char*)op.x + (some ? px[i] : 0u), some);
+      for (int i = 0; i < 2 * NT; ++i)
+        if (i * 4 < limit) copy16(dst + Z::A + place(i * 4 + lane / 8, lane % 8), px[i], bytes);
+    }
+  }
+  // 4 bits: the lane's columns 8 * (lane % 4) and on of each 32, of half a chunk, of token lane / 4.
+  __device__ __forceinline__ void fetch_tokens(int half, uint4 (&b)[NT][4]) const {
+    const int c = m_chunk * F::COLS + half * HALF;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint4* from = reinterpret_cast<const uint4*>(m_x[t] + c);
+      if (c + HALF <= op.C) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[t][k] = KIND == kRsSum ? __ldcg(from + 4 * k) : __ldg(from + 4 * k);  // (kRsSum: written by this launch)
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          b[t][k] = make_uint4(0, 0, 0, 0);
+          if (c + 32 * k < op.C) b[t][k] = KIND == kRsSum ? __ldcg(from + 4 * k) : __ldg(from + 4 * k);
+        }
+      }
     }
   }
 
-  // One stage's products added to acc.  MT: 1 where the runs have at most 8 rows, else 2.  odd0, odd1: bit q, whether the runs'
-  // scales of group q begin in the second half of their first word.  (Slots without a token hold anything: their sums are not read.)
+  // A stage's products added to acc.  MT: 1 where the runs have at most 8 rows, else 2.  (Slots without a token hold anything: their
+  // sums are not read.)
   template <int MT>
-  __device__ __forceinline__ void multiply(uint32_t a, int tokens, unsigned odd0, unsigned odd1, float (&acc)[REGS]) const {
-    const uint32_t x = a + Z::A;
+  __device__ __forceinline__ void multiply(uint32_t a, int tokens) {
     if constexpr (!kMma) {
       float w[32];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + lane * F::ROW + row_unit(lane, c) * 16), w + 4 * c);
+      for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + place(lane, c)), w + 4 * c);
 #pragma unroll
       for (int t = 0; t < SLOTS; ++t) {
         if (t >= tokens) break;
@@ -294,7 +325,7 @@ struct RowStream {
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           float v[4];
-          Vec16<float>::unpack(lds128(x + t * F::XROW + token_unit(t, c) * 16), v);
+          Vec16<float>::unpack(lds128(a + Z::A + place(t, c)), v);
           s0 = __fmaf_rn(w[4 * c], v[0], s0);
           s1 = __fmaf_rn(w[4 * c + 1], v[1], s1);
           s0 = __fmaf_rn(w[4 * c + 2], v[2], s0);
@@ -302,78 +333,95 @@ struct RowStream {
         }
         acc[t] += s0 + s1;
       }
-    } else if constexpr (!k4Bit) {
+    } else {
       uint32_t b[NT][4][2];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t r[4];
-          ldsm4(x + (8 * t + lane % 8) * F::XROW + token_unit(lane % 8, 4 * q + lane / 8) * 16, r);
+          ldsm4(a + Z::A + 8 * t * kRsRowBytes + place(lane % 8, 4 * q + lane / 8), r);
           b[t][2 * q][0] = r[0]; b[t][2 * q][1] = r[1]; b[t][2 * q + 1][0] = r[2]; b[t][2 * q + 1][1] = r[3];
         }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
           uint32_t w[4];
-          ldsm4(a + r * F::ROW + row_unit(r, 2 * k + lane / 16) * 16, w);
+          ldsm4(a + (lane / 8 % 2 * kRsRun + 8 * m) * kRsRowBytes + place(lane % 8, 2 * k + lane / 16), w);
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-            mma16816(reinterpret_cast<float(&)[4]>(acc[(m * NT + t) * 4]), w[0], w[1], w[2], w[3], b[t][k][0], b[t][k][1]);
+          for (int t = 0; t < NT; ++t) mma16816(sums(m, t), w[0], w[1], w[2], w[3], b[t][k][0], b[t][k][1]);
         }
-    } else {
-      const uint32_t sc = x + Z::X;
-      constexpr int per_group = F::GROUP / 32;  // 32-column units
-      float part[MT][NT][4];
+    }
+  }
+  __device__ __forceinline__ float (&sums(int m, int t))[4] { return reinterpret_cast<float(&)[4]>(acc[(m * NT + t) * 4]); }
+
+  // Half a stage's products on 4-bit rows.  at: the lane's first row address (ldmatrix); s0, s1: of the runs' scales of the half's
+  // groups 0, 2, ..; f0, f1: 2 or 0 bytes, to be flipped for groups 1, 3, ..
+  template <int MT>
+  __device__ __forceinline__ void multiply4(uint32_t at, const uint4 (&b)[NT][4], uint32_t s0, uint32_t s1, uint32_t f0, uint32_t f1) {
+    constexpr int per_group = F::GROUP / 32;  // 32-column units
+    float part[MT][NT][4];
+    uint32_t w[MT][4];
 #pragma unroll
-      for (int h = 0; h < F::COLS / 64; ++h) {  // 64 columns each
-        uint32_t w[MT][4];
+    for (int k = 0; k < 4; ++k) {
+      if (k % 2 == 0) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) ldsm4((k == 0 ? at : at ^ 32u) + 8 * m * kRsRowBytes, w[m]);  // (stages are 128-byte aligned)
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        uint32_t d0[4], d1[4];
+        dequantise(w[m][k % 2 * 2], d0);
+        dequantise(w[m][k % 2 * 2 + 1], d1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          if (k % per_group == 0) mma16816_first(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t][k].x, b[t][k].y);
+          else mma16816(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t][k].x, b[t][k].y);
+          mma16816(part[m][t], d0[2], d1[2], d0[3], d1[3], b[t][k].z, b[t][k].w);
+        }
+      }
+      if ((k + 1) % per_group == 0) {   // the group's sums, scaled once
+        const int q = k / per_group;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          const int r = (lane / 8 % 2) * kRsRun + 8 * m + lane % 8;
-          ldsm4(a + r * F::ROW + row_unit(r, 2 * h + lane / 16) * 16, w[m]);
-        }
+          const float e0 = scale(s0 + q * 72 + 16 * m + (q % 2 ? f0 : 0)), e1 = scale(s1 + q * 72 + 16 * m + (q % 2 ? f1 : 0));
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int k = 2 * h + v;          // 32-column unit
-          if (k % per_group == 0) {
-#pragma unroll
-            for (int j = 0; j < 4 * MT * NT; ++j) part[j / (4 * NT)][j / 4 % NT][j % 4] = 0.0f;
-          }
-          uint4 b[NT];
-#pragma unroll
-          for (int t = 0; t < NT; ++t) b[t] = lds128(x + (8 * t + lane / 4) * F::XROW + token_unit(lane / 4, 4 * k + lane % 4) * 16);
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            uint32_t d0[4], d1[4];
-            dequantise(w[m][2 * v], d0);
-            dequantise(w[m][2 * v + 1], d1);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              mma16816(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t].x, b[t].y);
-              mma16816(part[m][t], d0[2], d1[2], d0[3], d1[3], b[t].z, b[t].w);
-            }
-          }
-          if ((k + 1) % per_group == 0) {   // the group's sums, scaled once
-            const int q = k / per_group;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-              const float f0 = scale(sc, 2 * q, 8 * m + lane / 4 + ((odd0 >> q) & 1));
-              const float f1 = scale(sc, 2 * q + 1, 8 * m + lane / 4 + ((odd1 >> q) & 1));
-#pragma unroll
-              for (int t = 0; t < NT; ++t) {
-                float* s = acc + (m * NT + t) * 4;
-                s[0] = __fmaf_rn(f0, part[m][t][0], s[0]);
-                s[1] = __fmaf_rn(f0, part[m][t][1], s[1]);
-                s[2] = __fmaf_rn(f1, part[m][t][2], s[2]);
-                s[3] = __fmaf_rn(f1, part[m][t][3], s[3]);
-              }
-            }
+          for (int t = 0; t < NT; ++t) {
+            float(&s)[4] = sums(m, t);
+            s[0] = __fmaf_rn(e0, part[m][t][0], s[0]);
+            s[1] = __fmaf_rn(e0, part[m][t][1], s[1]);
+            s[2] = __fmaf_rn(e1, part[m][t][2], s[2]);
+            s[3] = __fmaf_rn(e1, part[m][t][3], s[3]);
           }
         }
       }
+    }
+  }
+  __device__ __forceinline__ void multiply_codes(uint32_t a) {
+    const uint32_t at = a + (lane / 8 % 2 * kRsRun) * kRsRowBytes + place(lane % 8, lane / 16), sc = a + Z::A + lane / 4 * 2;
+    // a run's scale of group g is number (matrix's + g) * N + row: whether it lies in the second half of its first word
+    uint32_t o0 = m_row & 1 ? 2u : 0u, o1 = row1(m_row, m_n0) & 1 ? 2u : 0u, flip = 0;
+    if (op.N & 1) {
+      flip = 2;
+      if ((m_base + m_chunk * F::GROUPS) & 1) { o0 ^= 2u; o1 ^= 2u; }
+    }
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      if (m_chunk * F::COLS + half * HALF >= op.C) break;
+      uint4 b[NT][4];
+      fetch_tokens(half, b);
+      if (half == 0) {
+        copies_wait<Z::STAGES - 1>();
+        __syncwarp();
+      } else if (F::GROUPS == 2) {  // (an odd number of groups on)
+        o0 ^= flip;
+        o1 ^= flip;
+      }
+      const uint32_t s0 = sc + half * (F::GROUPS * 36) + o0, s1 = sc + half * (F::GROUPS * 36) + 36 + o1;
+      const uint32_t f0 = flip == 0 ? 0 : o0 ? (uint32_t)-2 : 2, f1 = flip == 0 ? 0 : o1 ? (uint32_t)-2 : 2;
+      if (m_n0 > 8) multiply4<2>(at ^ (half * 64), b, s0, s1, f0, f1);
+      else multiply4<1>(at ^ (half * 64), b, s0, s1, f0, f1);
     }
   }
   // Eight codes as exact bf16 integers code - 8, in pairs of neighbouring columns: 128 + code has the code in its last bits.
@@ -387,9 +435,9 @@ struct RowStream {
       d[i] = *reinterpret_cast<const uint32_t*>(&r);
     }
   }
-  __device__ __forceinline__ static float scale(uint32_t sc, int pair, int i) {
+  __device__ __forceinline__ static float scale(uint32_t at) {
     unsigned short v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(sc + pair * 36 + i * 2) : "memory");
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at) : "memory");
     return __uint_as_float((uint32_t)v << 16);
   }
 
@@ -397,6 +445,7 @@ struct RowStream {
 
   // Where the products are; what run() leaves of a tile that goes on in the next warps' shares.
   int m_tile, m_u, m_chunk, m_row, m_n0, m_n1, m_base, m_tokens;
+  const X* m_x[NT];  // (4 bits) the lane's first column of its tokens
   bool pending;
   float acc[REGS];
 
@@ -404,7 +453,7 @@ struct RowStream {
     __syncwarp();
 #pragma unroll 1
     for (int i = 0; i < Z::STAGES - 1; ++i)
-      if (unit < unit_end) {
+      if (left > 0) {
         copy_weights(ring + i * Z::STAGE);
         advance();
       }
@@ -413,6 +462,9 @@ struct RowStream {
 
   __device__ __forceinline__ void set_matrix() {
     m_tokens = list.count[m_u];
+    if constexpr (k4Bit)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) m_x[t] = (const X*)op.x + (long long)x_row(m_u, 8 * t + lane / 4) * op.C + lane % 4 * 8;
     if constexpr (k4Bit) m_base = list.used[m_u] * (op.C / F::GROUP);
   }
   // kRsSum: where a warp adds up its rows' results per token.  (The rows are swizzled so that the lanes of a fragment, which
@@ -425,7 +477,6 @@ struct RowStream {
   template <typename Weight, typename Finish>
   __device__ __forceinline__ void run(RowStream* start, float* slots, Weight weight, Finish finish) {
     const RowStream& at = start != nullptr ? *start : *this;
-    const int total = (int)(at.unit_end - at.unit);
     m_tile = at.tile_i; m_u = at.u; m_chunk = at.chunk; m_row = at.row; m_n0 = at.n0; m_n1 = at.n1;
     pending = false;
     if (total <= 0) {
@@ -459,22 +510,20 @@ struct RowStream {
 #pragma unroll 1
     for (int i = 0; i < total; ++i) {
       __syncwarp();
-      if (unit < unit_end) {
+      if (left > 0) {
         copy_weights(next);
         copy_tokens(next);
         advance();
       }
       copies_commit();
-      copies_wait<Z::STAGES - 1>();
-      __syncwarp();
-      unsigned odd0 = 0, odd1 = 0;
-      if constexpr (k4Bit) {  // scale number (matrix's + group) * N + row
-        const unsigned swing = op.N & 1 ? 0xaau ^ ((m_base + m_chunk * F::GROUPS) & 1 ? 0xffu : 0u) : 0u;
-        odd0 = swing ^ (m_row & 1 ? 0xffu : 0u);
-        odd1 = swing ^ (row1(m_row, m_n0) & 1 ? 0xffu : 0u);
+      if constexpr (k4Bit) {
+        multiply_codes(stage);
+      } else {
+        copies_wait<Z::STAGES - 1>();
+        __syncwarp();
+        if (m_n0 > 8) multiply<2>(stage, m_tokens);
+        else multiply<1>(stage, m_tokens);
       }
-      if (m_n0 > 8) multiply<2>(stage, m_tokens, odd0, odd1, acc);
-      else multiply<1>(stage, m_tokens, odd0, odd1, acc);
       next = stage;
       stage = stage + Z::STAGE == ring + Z::STAGES * Z::STAGE ? ring : stage + Z::STAGE;
       ++m_chunk;
