@@ -4,88 +4,161 @@
 
 namespace moehub {
 
+// ---- packing and unpacking: bound by HBM; a warp (of short rows: a part of one) walks along a row, so that a row's place is
+// worked out once, with kPackUnroll words of eight columns per lane in flight ------------------------------------------------------
 constexpr int kPackThreads = 256;
+constexpr int kPackUnroll = 4;
 
-template <typename T> __device__ __forceinline__ void load8(const T* p, float (&v)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
-  Vec16<float>::unpack(__ldcs(reinterpret_cast<const uint4*>(p)), v);
-  Vec16<float>::unpack(__ldcs(reinterpret_cast<const uint4*>(p) + 1), v + 4);
+template <typename T> struct Eight;  // eight columns
+template <> struct Eight<float> {
+  uint4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+    v[1] = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+  }
+  __device__ __forceinline__ void floats(float (&f)[8]) const {
+    Vec16<float>::unpack(v[0], f);
+    Vec16<float>::unpack(v[1], f + 4);
+  }
+};
+template <> struct Eight<__nv_bfloat16> {
+  uint4 v[1];
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v[0] = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void floats(float (&f)[8]) const { Vec16<__nv_bfloat16>::unpack(v[0], f); }
+};
+
+// The code of w (the nearest integer to w / s, ties to even, within -8..7, plus 8); inverse: 1 / s.  A product with the inverse and one
+// correction give the quotient rounded to fp32, which is exact where w / s lies on the border between two codes.  Where w is a
+// bf16 number it is nowhere else on a border ((2 k + 1) s / 2 has 12 bits, w 8: they are equal, or 2^-13 apart); where w is an fp32 number
+// the decision is left to the remainder w - k s, which is exact: k s has 12 bits and lies within s of w.
+template <bool BF16>
+__device__ __forceinline__ uint32_t w4_code(float w, float s, float inverse) {
+  const float near = w * inverse;
+  const float quotient = __fmaf_rn(__fmaf_rn(-near, s, w), inverse, near);
+  constexpr float kIntegers = 12582912.0f;  // 1.5 * 2^23: a sum with it is an integer, in the last bits
+  float sum = quotient + (kIntegers + 8.0f);
+  if (!BF16) {
+    const float k = sum - (kIntegers + 8.0f), r = __fmaf_rn(-k, s, w), half = 0.5f * s;
+    const bool odd = __float_as_uint(sum) & 1u;
+    if (fabsf(r) > half || (fabsf(r) == half && odd)) sum += r > 0.0f ? 1.0f : -1.0f;
+  }
+  return min(__float_as_uint(sum) - 0x4b400000u, 15u);  // (the largest quotient is 7 and what the scale was rounded by)
 }
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float (&v)[8]) {
-  Vec16<__nv_bfloat16>::unpack(__ldcs(reinterpret_cast<const uint4*>(p)), v);
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&v)[8]);
-template <> __device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
-  __stcs(reinterpret_cast<uint4*>(p), Vec16<float>::pack(v));
-  __stcs(reinterpret_cast<uint4*>(p) + 1, Vec16<float>::pack(v + 4));
-}
-template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, const float (&v)[8]) {
-  __stcs(reinterpret_cast<uint4*>(p), Vec16<__nv_bfloat16>::pack(v));
+// The same without assuming that s has an inverse.
+__device__ __noinline__ uint32_t w4_code_tiny(float w, float s) {
+  const double q = rint((double)w / (double)s);
+  return (uint32_t)(int)(fmin(fmax(q, -8.0), 7.0) + 8.0);
 }
 
-// The code of w (the nearest integer to w / s, ties to even, within -8..7, plus 8).  The quotient in fp32 can land on the
-// border between two integers without w doing so, so the decision is left to the remainder w - k s: k s has at most 12 bits and
-// lies within s of w, so the fused multiply-add gives it exactly.
-__device__ __forceinline__ uint32_t w4_code(float w, float s) {
-  if (!(s > 0.0f) || !(s < INFINITY)) return 8u;
-  const float k = rintf(fminf(fmaxf(w / s, -9.0f), 9.0f));
-  const float r = __fmaf_rn(-k, s, w), half = 0.5f * s;
-  int q = (int)k;
-  if (r > half || (r == half && (q & 1))) q += 1;
-  if (r < -half || (r == -half && (q & 1))) q -= 1;
-  return (uint32_t)(min(max(q, -8), 7) + 8);
-}
+struct PackRows {
+  long long rows;  // of all the matrices
+  int N, C, lanes; // lanes: per row, a power of two
+};
 
-// A thread takes the eight columns of a word, neighbouring threads neighbouring words of a row; the G / 8 threads of a group
-// find its largest magnitude together.
 template <typename T, int G>
 __global__ void __launch_bounds__(kPackThreads)
-w4_pack_kernel(const T* __restrict__ w, size_t words, int N, int C, uint32_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales) {
-  constexpr int LANES = G / 8;
-  const int per_row = C / 8;
-  for (size_t i0 = (size_t)blockIdx.x * kPackThreads; i0 < words; i0 += (size_t)gridDim.x * kPackThreads) {
-    const size_t i = i0 + threadIdx.x;
-    const bool live = i < words;  // (whole groups: words is a multiple of LANES)
-    float v[8];
-    if (live) load8(w + i * 8, v);
-    float largest = 0.0f;
-    bool fine = true;
+w4_pack_kernel(const T* __restrict__ w, const PackRows p, uint32_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales) {
+  constexpr int LANES = G / 8;  // of a group
+  const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
+  const long long step = (long long)gridDim.x * kPackThreads / p.lanes;
+  for (long long r0 = ((long long)blockIdx.x * kPackThreads + threadIdx.x) / p.lanes;; r0 += step) {
+    const bool live = r0 < p.rows;
+    if (!__any_sync(0xffffffffu, live)) break;
+    const long long row = live ? r0 : 0;
+    const long long e = row / p.N;
+    const int n = (int)(row - e * p.N);
+    const T* from = w + row * p.C;
+    for (int i0 = lane; i0 - lane < per_row; i0 += p.lanes * kPackUnroll) {
+      Eight<T> raw[kPackUnroll];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (!live) v[j] = 0.0f;
-      largest = fmaxf(largest, fabsf(v[j]));
-      fine = fine && fabsf(v[j]) < INFINITY;
-    }
-    if (!fine) largest = INFINITY;  // a NaN or an infinity: the group's scale is NaN
+      for (int j = 0; j < kPackUnroll; ++j)
+        if (live && i0 + j * p.lanes < per_row) raw[j].load(from + (size_t)(i0 + j * p.lanes) * 8);
 #pragma unroll
-    for (int off = LANES / 2; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
-    const __nv_bfloat16 scale = __float2bfloat16_rn(largest < INFINITY ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
-    if (!live) continue;
-    uint32_t word = 0;
+      for (int j = 0; j < kPackUnroll; ++j) {
+        const int i = i0 + j * p.lanes;
+        const bool mine = live && i < per_row;  // (whole groups: per_row is a multiple of LANES)
+        float v[8], largest = 0.0f;
+        if (mine) raw[j].floats(v);
+        bool fine = true;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) word |= w4_code(v[j], __bfloat162float(scale)) << w4_shift(j);
-    codes[i] = word;
-    if (threadIdx.x % LANES == 0) {
-      const size_t row = i / per_row;  // of all the experts' rows
-      const int g = (int)(i % per_row) / LANES;
-      scales[(row / N * (C / G) + g) * N + row % N] = scale;
+        for (int c = 0; c < 8; ++c) {
+          if (!mine) v[c] = 0.0f;
+          largest = fmaxf(largest, fabsf(v[c]));
+          fine = fine && !isnan(v[c]);
+        }
+        if (!fine) largest = INFINITY;  // a NaN or an infinity: the group's scale is NaN
+#pragma unroll
+        for (int off = LANES / 2; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
+        const __nv_bfloat16 scale = __float2bfloat16_rn(largest < INFINITY ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
+        if (!mine) continue;
+        const float s = __bfloat162float(scale);
+        uint32_t word = 0x88888888u;  // scale 0 or NaN
+        if (s >= 1e-30f) {
+          const float inverse = __frcp_rn(s);
+          word = 0;
+#pragma unroll
+          for (int c = 0; c < 8; ++c) word |= w4_code<sizeof(T) == 2>(v[c], s, inverse) << w4_shift(c);
+        } else if (s > 0.0f) {
+          word = 0;
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) word |= w4_code_tiny(v[c], s) << w4_shift(c);
+        }
+        __stcs(codes + row * per_row + i, word);
+        if (i % LANES == 0) scales[(e * (p.C / G) + i / LANES) * p.N + n] = scale;
+      }
     }
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kPackThreads)
-w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __restrict__ scales, size_t words, int N, int C, int G, T* __restrict__ w) {
-  const int per_row = C / 8, per_group = G / 8;
-  for (size_t i = (size_t)blockIdx.x * kPackThreads + threadIdx.x; i < words; i += (size_t)gridDim.x * kPackThreads) {
-    const size_t row = i / per_row;
-    const int g = (int)(i % per_row) / per_group;
-    const float scale = __bfloat162float(scales[(row / N * (C / G) + g) * N + row % N]);
-    const uint32_t word = __ldcs(codes + i);
-    float v[8];
+// Eight codes times their scale, rounded once.
+__device__ __forceinline__ void w4_unpack8(uint32_t word, __nv_bfloat16 scale, __nv_bfloat16* to) {
+  const __nv_bfloat162 s = __halves2bfloat162(scale, scale), bias = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));  // 136
+  uint32_t d[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = scale * w4_value(word, j);
-    store8(w + i * 8, v);
+  for (int i = 0; i < 4; ++i) {  // columns 2 i and 2 i + 1: 128 + code, less 136
+    const uint32_t v = ((word >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+    const __nv_bfloat162 r = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), bias), s);
+    d[i] = *reinterpret_cast<const uint32_t*>(&r);
+  }
+  __stcs(reinterpret_cast<uint4*>(to), make_uint4(d[0], d[1], d[2], d[3]));
+}
+__device__ __forceinline__ void w4_unpack8(uint32_t word, __nv_bfloat16 scale, float* to) {
+  const float s = __bfloat162float(scale);
+  float v[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) v[c] = s * w4_value(word, c);
+  __stcs(reinterpret_cast<uint4*>(to), Vec16<float>::pack(v));
+  __stcs(reinterpret_cast<uint4*>(to) + 1, Vec16<float>::pack(v + 4));
+}
+
+template <typename T, int G>
+__global__ void __launch_bounds__(kPackThreads)
+w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __restrict__ scales, const PackRows p, T* __restrict__ w) {
+  constexpr int LANES = G / 8;
+  const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
+  const long long step = (long long)gridDim.x * kPackThreads / p.lanes;
+  for (long long row = ((long long)blockIdx.x * kPackThreads + threadIdx.x) / p.lanes; row < p.rows; row += step) {
+    const long long e = row / p.N;
+    const uint32_t* from = codes + row * per_row;
+    const __nv_bfloat16* scale = scales + e * (p.C / G) * p.N + (row - e * p.N);
+    T* to = w + row * p.C;
+    for (int i0 = lane; i0 < per_row; i0 += p.lanes * kPackUnroll) {
+      uint32_t word[kPackUnroll];
+      __nv_bfloat16 s[kPackUnroll];
+#pragma unroll
+      for (int j = 0; j < kPackUnroll; ++j) {
+        const int i = i0 + j * p.lanes;
+        if (i < per_row) {
+          word[j] = __ldcs(from + i);
+          s[j] = scale[(size_t)(i / LANES) * p.N];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kPackUnroll; ++j) {
+        const int i = i0 + j * p.lanes;
+        if (i < per_row) w4_unpack8(word[j], s[j], to + (size_t)i * 8);
+      }
+    }
   }
 }
 
@@ -95,26 +168,34 @@ static int sm_count_now() {
   return sms;
 }
 
-static int pack_grid(size_t words) {
-  const size_t want = (words + kPackThreads - 1) / kPackThreads;
-  const size_t most = (size_t)sm_count_now() * 8;
+// Rows and lanes per row (at least a group's); returns the grid, 0 on a CUDA error.
+static int pack_rows(int experts, int N, int C, int group, PackRows& p) {
+  p.rows = (long long)experts * N;
+  p.N = N;
+  p.C = C;
+  p.lanes = group / 8;
+  while (p.lanes < 32 && p.lanes < C / 8) p.lanes *= 2;
+  const long long want = (p.rows * p.lanes + kPackThreads - 1) / kPackThreads, most = (long long)sm_count_now() * 8;
   return (int)(want < most ? want : most);
 }
 
 template <typename T>
-static cudaError_t launch_pack(const void* w, size_t words, int N, int C, int group, const moe_w4_t& out, cudaStream_t st) {
-  const int grid = pack_grid(words);
+static cudaError_t launch_pack(const void* w, int experts, int N, int C, int group, const moe_w4_t& out, cudaStream_t st) {
+  PackRows p;
+  const int grid = pack_rows(experts, N, C, group, p);
   if (grid <= 0) return cudaErrorUnknown;
   auto kern = group == 32 ? w4_pack_kernel<T, 32> : group == 64 ? w4_pack_kernel<T, 64> : w4_pack_kernel<T, 128>;
-  kern<<<grid, kPackThreads, 0, st>>>((const T*)w, words, N, C, (uint32_t*)out.codes, (__nv_bfloat16*)out.scales);
+  kern<<<grid, kPackThreads, 0, st>>>((const T*)w, p, (uint32_t*)out.codes, (__nv_bfloat16*)out.scales);
   return cudaGetLastError();
 }
 
 template <typename T>
-static cudaError_t launch_unpack(const moe_w4_t& w, size_t words, int N, int C, int group, void* out, cudaStream_t st) {
-  const int grid = pack_grid(words);
+static cudaError_t launch_unpack(const moe_w4_t& w, int experts, int N, int C, int group, void* out, cudaStream_t st) {
+  PackRows p;
+  const int grid = pack_rows(experts, N, C, group, p);
   if (grid <= 0) return cudaErrorUnknown;
-  w4_unpack_kernel<T><<<grid, kPackThreads, 0, st>>>((const uint32_t*)w.codes, (const __nv_bfloat16*)w.scales, words, N, C, group, (T*)out);
+  auto kern = group == 32 ? w4_unpack_kernel<T, 32> : group == 64 ? w4_unpack_kernel<T, 64> : w4_unpack_kernel<T, 128>;
+  kern<<<grid, kPackThreads, 0, st>>>((const uint32_t*)w.codes, (const __nv_bfloat16*)w.scales, p, (T*)out);
   return cudaGetLastError();
 }
 
@@ -208,9 +289,8 @@ int moe_w4_pack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t gr
   if (rc != MOE_OK) return rc;
   if (!d_w) return MOE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(d_w) & 15) return MOE_ERR_ALIGN;
-  const size_t words = (size_t)experts * N * (C / 8);
-  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_pack<float>(d_w, words, N, C, group, *out, (cudaStream_t)stream)
-                                          : launch_pack<__nv_bfloat16>(d_w, words, N, C, group, *out, (cudaStream_t)stream);
+  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_pack<float>(d_w, experts, N, C, group, *out, (cudaStream_t)stream)
+                                          : launch_pack<__nv_bfloat16>(d_w, experts, N, C, group, *out, (cudaStream_t)stream);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -220,9 +300,8 @@ int moe_w4_unpack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t 
   if (rc != MOE_OK) return rc;
   if (!d_out) return MOE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(d_out) & 15) return MOE_ERR_ALIGN;
-  const size_t words = (size_t)experts * N * (C / 8);
-  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_unpack<float>(*w, words, N, C, group, d_out, (cudaStream_t)stream)
-                                          : launch_unpack<__nv_bfloat16>(*w, words, N, C, group, d_out, (cudaStream_t)stream);
+  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_unpack<float>(*w, experts, N, C, group, d_out, (cudaStream_t)stream)
+                                          : launch_unpack<__nv_bfloat16>(*w, experts, N, C, group, d_out, (cudaStream_t)stream);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
