@@ -4,10 +4,38 @@
 
 namespace moehub {
 
-// ---- packing and unpacking: bound by HBM; a warp (of short rows: a part of one) walks along a row, so that a row's place is
-// worked out once, with kPackUnroll words of eight columns per lane in flight ------------------------------------------------------
+// ---- packing and unpacking ---------------------------------------------------------------------------------------------------
+// A warp takes a segment of a row (rows of few words: several), kPackUnroll words of eight columns per lane in flight, and is done: rows,
+// segments and matrices are the grid's three dimensions, so that no place has to be divided out and small matrices fill the GPU.
 constexpr int kPackThreads = 256;
 constexpr int kPackUnroll = 4;
+
+struct PackShape {
+  int experts, N, C, lanes;  // lanes: of a row's segment, a power of two
+};
+
+typedef unsigned long long f32x2;  // two fp32 numbers for the paired instructions
+__device__ __forceinline__ f32x2 pair(float a, float b) {
+  f32x2 d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
 template <typename T> struct Eight;  // eight columns
 template <> struct Eight<float> {
@@ -16,96 +44,112 @@ template <> struct Eight<float> {
     v[0] = __ldcs(reinterpret_cast<const uint4*>(p));
     v[1] = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
   }
-  __device__ __forceinline__ void floats(float (&f)[8]) const {
-    Vec16<float>::unpack(v[0], f);
-    Vec16<float>::unpack(v[1], f + 4);
+  __device__ __forceinline__ void clear() { v[0] = v[1] = make_uint4(0, 0, 0, 0); }
+  // The largest magnitude's bits: an infinity's or a NaN's are larger than any number's.
+  __device__ __forceinline__ uint32_t largest() const {
+    constexpr uint32_t m = 0x7fffffffu;
+    return max(max(max(v[0].x & m, v[0].y & m), max(v[0].z & m, v[0].w & m)), max(max(v[1].x & m, v[1].y & m), max(v[1].z & m, v[1].w & m)));
   }
+  __device__ __forceinline__ static uint32_t as_float(uint32_t key) { return key; }
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(reinterpret_cast<const uint32_t*>(v)[i]); }
 };
 template <> struct Eight<__nv_bfloat16> {
-  uint4 v[1];
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v[0] = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void floats(float (&f)[8]) const { Vec16<__nv_bfloat16>::unpack(v[0], f); }
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ uint32_t largest() const {
+    constexpr uint32_t m = 0x7fff7fffu;
+    const uint32_t two = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+    return max(two & 0xffffu, two >> 16);
+  }
+  __device__ __forceinline__ static uint32_t as_float(uint32_t key) { return key << 16; }
+  __device__ __forceinline__ float operator[](int i) const {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(&v)[i / 2];
+    return __uint_as_float(i % 2 ? w & 0xffff0000u : w << 16);
+  }
 };
 
-// The code of w (the nearest integer to w / s, ties to even, within -8..7, plus 8); inverse: 1 / s.  A product with the inverse and one
-// correction give the quotient rounded to fp32, which is exact where w / s lies on the border between two codes.  Where w is a
-// bf16 number it is nowhere else on a border ((2 k + 1) s / 2 has 12 bits, w 8: they are equal, or 2^-13 apart); where w is an fp32 number
-// the decision is left to the remainder w - k s, which is exact: k s has 12 bits and lies within s of w.
-template <bool BF16>
-__device__ __forceinline__ uint32_t w4_code(float w, float s, float inverse) {
-  const float near = w * inverse;
-  const float quotient = __fmaf_rn(__fmaf_rn(-near, s, w), inverse, near);
-  constexpr float kIntegers = 12582912.0f;  // 1.5 * 2^23: a sum with it is an integer, in the last bits
-  float sum = quotient + (kIntegers + 8.0f);
-  if (!BF16) {
-    const float k = sum - (kIntegers + 8.0f), r = __fmaf_rn(-k, s, w), half = 0.5f * s;
-    const bool odd = __float_as_uint(sum) & 1u;
-    if (fabsf(r) > half || (fabsf(r) == half && odd)) sum += r > 0.0f ? 1.0f : -1.0f;
-  }
-  return min(__float_as_uint(sum) - 0x4b400000u, 15u);  // (the largest quotient is 7 and what the scale was rounded by)
-}
-// The same without assuming that s has an inverse.
-__device__ __noinline__ uint32_t w4_code_tiny(float w, float s) {
+// The code of w without assumptions on s: the nearest integer to w / s, ties to even, within -8..7, plus 8; 8 without a scale.
+__device__ __noinline__ uint32_t w4_code(float w, float s) {
+  if (!(s > 0.0f)) return 8;
   const double q = rint((double)w / (double)s);
   return (uint32_t)(int)(fmin(fmax(q, -8.0), 7.0) + 8.0);
 }
-
-struct PackRows {
-  long long rows;  // of all the matrices
-  int N, C, lanes; // lanes: per row, a power of two
-};
+template <typename T>
+__device__ __forceinline__ uint32_t w4_word_slow(const Eight<T>& v, float s) {
+  uint32_t word = 0;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) word |= w4_code(v[c], s) << w4_shift(c);
+  return word;
+}
+// A word of codes, for a scale whose inverse is a number.  A product with the inverse and one correction (Markstein's) give the quotient rounded to fp32, also where the inverse is an ulp off; on the border
+// between two codes it is exact.  Where w is a bf16 number the quotient is nowhere else on a border: (2 k + 1) s / 2 has
+// 12 bits and w 8, so they are equal or 2^-12 of them apart.  Where w is an fp32 number it may be, and |w - k s|, which is exact (k s
+// has 12 bits and lies within s of w), is near s / 2 then: such words, one in a hundred thousand, are done with care.
+template <typename T>
+__device__ __forceinline__ uint32_t w4_word(const Eight<T>& v, float s) {
+  float inverse;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(inverse) : "f"(s));
+  constexpr float kIntegers = 12582912.0f + 8.0f;  // 1.5 * 2^23: a sum with it is an integer, in the last bits; and the code's 8
+  const f32x2 inverse2 = pair(inverse, inverse), minus2 = pair(-s, -s), integers2 = pair(kIntegers, kIntegers), back2 = pair(-kIntegers, -kIntegers);
+  uint32_t word = 0;
+  float farthest = 0.0f;
+#pragma unroll
+  for (int c = 0; c < 8; c += 2) {
+    const f32x2 w = pair(v[c], v[c + 1]);
+    const f32x2 near = mul2(w, inverse2);
+    const f32x2 sum = add2(fma2(fma2(near, minus2, w), inverse2, near), integers2);
+    float a, b;
+    unpair(sum, a, b);
+    word += __float_as_uint(a) * (1u << w4_shift(c)) + __float_as_uint(b) * (1u << w4_shift(c + 1));
+    if (sizeof(T) == 4) {
+      float r0, r1;
+      unpair(fma2(add2(sum, back2), minus2, w), r0, r1);
+      farthest = fmaxf(farthest, fmaxf(fabsf(r0), fabsf(r1)));
+    }
+  }
+  word -= 0x4b400000u * 0x11111111u;  // (the integers' own bits, at every code's place)
+  if (sizeof(T) == 4 && farthest > 0.4999f * s) return w4_word_slow(v, s);
+  return word;
+}
 
 template <typename T, int G>
-__global__ void __launch_bounds__(kPackThreads)
-w4_pack_kernel(const T* __restrict__ w, const PackRows p, uint32_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales) {
+__global__ void __launch_bounds__(kPackThreads, 4)
+w4_pack_kernel(const T* __restrict__ w, const PackShape p, uint32_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales) {
   constexpr int LANES = G / 8;  // of a group
   const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
-  const long long step = (long long)gridDim.x * kPackThreads / p.lanes;
-  for (long long r0 = ((long long)blockIdx.x * kPackThreads + threadIdx.x) / p.lanes;; r0 += step) {
-    const bool live = r0 < p.rows;
-    if (!__any_sync(0xffffffffu, live)) break;
-    const long long row = live ? r0 : 0;
-    const long long e = row / p.N;
-    const int n = (int)(row - e * p.N);
-    const T* from = w + row * p.C;
-    for (int i0 = lane; i0 - lane < per_row; i0 += p.lanes * kPackUnroll) {
-      Eight<T> raw[kPackUnroll];
+  const int n = blockIdx.x * (kPackThreads / p.lanes) + threadIdx.x / p.lanes;
+  const int i0 = blockIdx.y * (p.lanes * kPackUnroll) + lane;
+  for (int e = blockIdx.z; e < p.experts; e += gridDim.z) {
+    const size_t row = (size_t)e * p.N + n;
+    Eight<T> v[kPackUnroll];
 #pragma unroll
-      for (int j = 0; j < kPackUnroll; ++j)
-        if (live && i0 + j * p.lanes < per_row) raw[j].load(from + (size_t)(i0 + j * p.lanes) * 8);
+    for (int j = 0; j < kPackUnroll; ++j) {
+      v[j].clear();
+      if (n < p.N && i0 + j * p.lanes < per_row) v[j].load(w + row * p.C + (size_t)(i0 + j * p.lanes) * 8);
+    }
 #pragma unroll
-      for (int j = 0; j < kPackUnroll; ++j) {
-        const int i = i0 + j * p.lanes;
-        const bool mine = live && i < per_row;  // (whole groups: per_row is a multiple of LANES)
-        float v[8], largest = 0.0f;
-        if (mine) raw[j].floats(v);
-        bool fine = true;
+    for (int j = 0; j < kPackUnroll; ++j) {
+      const int i = i0 + j * p.lanes;
+      uint32_t key = v[j].largest();
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          if (!mine) v[c] = 0.0f;
-          largest = fmaxf(largest, fabsf(v[c]));
-          fine = fine && !isnan(v[c]);
-        }
-        if (!fine) largest = INFINITY;  // a NaN or an infinity: the group's scale is NaN
-#pragma unroll
-        for (int off = LANES / 2; off > 0; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, off));
-        const __nv_bfloat16 scale = __float2bfloat16_rn(largest < INFINITY ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
-        if (!mine) continue;
-        const float s = __bfloat162float(scale);
-        uint32_t word = 0x88888888u;  // scale 0 or NaN
-        if (s >= 1e-30f) {
-          const float inverse = __frcp_rn(s);
-          word = 0;
-#pragma unroll
-          for (int c = 0; c < 8; ++c) word |= w4_code<sizeof(T) == 2>(v[c], s, inverse) << w4_shift(c);
-        } else if (s > 0.0f) {
-          word = 0;
-#pragma unroll 1
-          for (int c = 0; c < 8; ++c) word |= w4_code_tiny(v[c], s) << w4_shift(c);
-        }
-        __stcs(codes + row * per_row + i, word);
-        if (i % LANES == 0) scales[(e * (p.C / G) + i / LANES) * p.N + n] = scale;
+      for (int off = LANES / 2; off > 0; off >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, off));
+      if (n >= p.N || i >= per_row) continue;  // (whole groups: per_row is a multiple of LANES)
+      const uint32_t bits = Eight<T>::as_float(key);
+      const float largest = __uint_as_float(bits);
+      __nv_bfloat16 scale;
+      uint32_t word;
+      if (largest > 1e-28f && bits < 0x7f800000u) {
+        constexpr float seventh = 1.0f / 7.0f;  // (the quotient rounded to fp32, as in w4_word)
+        const float near = largest * seventh;
+        scale = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-near, 7.0f, largest), seventh, near));
+        word = w4_word(v[j], __bfloat162float(scale));
+      } else {  // zeros, tiny numbers; a NaN or an infinity: NaN
+        scale = __float2bfloat16_rn(bits < 0x7f800000u ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
+        word = w4_word_slow(v[j], __bfloat162float(scale));
       }
+      __stcs(codes + row * per_row + i, word);
+      if (i % LANES == 0) scales[((size_t)e * (p.C / G) + i / LANES) * p.N + n] = scale;
     }
   }
 }
@@ -133,70 +177,60 @@ __device__ __forceinline__ void w4_unpack8(uint32_t word, __nv_bfloat16 scale, f
 
 template <typename T, int G>
 __global__ void __launch_bounds__(kPackThreads)
-w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __restrict__ scales, const PackRows p, T* __restrict__ w) {
+w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __restrict__ scales, const PackShape p, T* __restrict__ w) {
   constexpr int LANES = G / 8;
   const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
-  const long long step = (long long)gridDim.x * kPackThreads / p.lanes;
-  for (long long row = ((long long)blockIdx.x * kPackThreads + threadIdx.x) / p.lanes; row < p.rows; row += step) {
-    const long long e = row / p.N;
-    const uint32_t* from = codes + row * per_row;
-    const __nv_bfloat16* scale = scales + e * (p.C / G) * p.N + (row - e * p.N);
-    T* to = w + row * p.C;
-    for (int i0 = lane; i0 < per_row; i0 += p.lanes * kPackUnroll) {
-      uint32_t word[kPackUnroll];
-      __nv_bfloat16 s[kPackUnroll];
+  const int n = blockIdx.x * (kPackThreads / p.lanes) + threadIdx.x / p.lanes;
+  const int i0 = blockIdx.y * (p.lanes * kPackUnroll) + lane;
+  if (n >= p.N) return;
+  for (int e = blockIdx.z; e < p.experts; e += gridDim.z) {
+    const size_t row = (size_t)e * p.N + n;
+    uint32_t word[kPackUnroll];
+    __nv_bfloat16 s[kPackUnroll];
 #pragma unroll
-      for (int j = 0; j < kPackUnroll; ++j) {
-        const int i = i0 + j * p.lanes;
-        if (i < per_row) {
-          word[j] = __ldcs(from + i);
-          s[j] = scale[(size_t)(i / LANES) * p.N];
-        }
+    for (int j = 0; j < kPackUnroll; ++j) {
+      const int i = i0 + j * p.lanes;
+      if (i < per_row) {
+        word[j] = __ldcs(codes + row * per_row + i);
+        s[j] = scales[((size_t)e * (p.C / G) + i / LANES) * p.N + n];
       }
+    }
 #pragma unroll
-      for (int j = 0; j < kPackUnroll; ++j) {
-        const int i = i0 + j * p.lanes;
-        if (i < per_row) w4_unpack8(word[j], s[j], to + (size_t)i * 8);
-      }
+    for (int j = 0; j < kPackUnroll; ++j) {
+      const int i = i0 + j * p.lanes;
+      if (i < per_row) w4_unpack8(word[j], s[j], w + row * p.C + (size_t)i * 8);
     }
   }
 }
 
-static int sm_count_now() {
-  int device = 0, sms = 0;
-  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
-  return sms;
-}
-
-// Rows and lanes per row (at least a group's); returns the grid, 0 on a CUDA error.
-static int pack_rows(int experts, int N, int C, int group, PackRows& p) {
-  p.rows = (long long)experts * N;
-  p.N = N;
-  p.C = C;
+// The grid, and the lanes of a row's segment (at least a group's).
+static dim3 pack_grid(PackShape& p, int group) {
   p.lanes = group / 8;
-  while (p.lanes < 32 && p.lanes < C / 8) p.lanes *= 2;
-  const long long want = (p.rows * p.lanes + kPackThreads - 1) / kPackThreads, most = (long long)sm_count_now() * 8;
-  return (int)(want < most ? want : most);
+  while (p.lanes < 32 && p.lanes < p.C / 8) p.lanes *= 2;
+  const int rows = kPackThreads / p.lanes, words = p.lanes * kPackUnroll;
+  return dim3((p.N + rows - 1) / rows, (p.C / 8 + words - 1) / words, p.experts < 65535 ? p.experts : 65535);
 }
 
 template <typename T>
-static cudaError_t launch_pack(const void* w, int experts, int N, int C, int group, const moe_w4_t& out, cudaStream_t st) {
-  PackRows p;
-  const int grid = pack_rows(experts, N, C, group, p);
-  if (grid <= 0) return cudaErrorUnknown;
+static cudaError_t launch_pack(const void* w, PackShape p, int group, const moe_w4_t& out, cudaStream_t st) {
+  const dim3 grid = pack_grid(p, group);
   auto kern = group == 32 ? w4_pack_kernel<T, 32> : group == 64 ? w4_pack_kernel<T, 64> : w4_pack_kernel<T, 128>;
   kern<<<grid, kPackThreads, 0, st>>>((const T*)w, p, (uint32_t*)out.codes, (__nv_bfloat16*)out.scales);
   return cudaGetLastError();
 }
 
 template <typename T>
-static cudaError_t launch_unpack(const moe_w4_t& w, int experts, int N, int C, int group, void* out, cudaStream_t st) {
-  PackRows p;
-  const int grid = pack_rows(experts, N, C, group, p);
-  if (grid <= 0) return cudaErrorUnknown;
+static cudaError_t launch_unpack(const moe_w4_t& w, PackShape p, int group, void* out, cudaStream_t st) {
+  const dim3 grid = pack_grid(p, group);
   auto kern = group == 32 ? w4_unpack_kernel<T, 32> : group == 64 ? w4_unpack_kernel<T, 64> : w4_unpack_kernel<T, 128>;
   kern<<<grid, kPackThreads, 0, st>>>((const uint32_t*)w.codes, (const __nv_bfloat16*)w.scales, p, (T*)out);
   return cudaGetLastError();
+}
+
+static int sm_count_now() {
+  int device = 0, sms = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+  return sms;
 }
 
 // ---- products with a few rows ------------------------------------------------------------------------------------------------
@@ -289,8 +323,8 @@ int moe_w4_pack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t gr
   if (rc != MOE_OK) return rc;
   if (!d_w) return MOE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(d_w) & 15) return MOE_ERR_ALIGN;
-  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_pack<float>(d_w, experts, N, C, group, *out, (cudaStream_t)stream)
-                                          : launch_pack<__nv_bfloat16>(d_w, experts, N, C, group, *out, (cudaStream_t)stream);
+  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_pack<float>(d_w, PackShape{experts, N, C, 0}, group, *out, (cudaStream_t)stream)
+                                          : launch_pack<__nv_bfloat16>(d_w, PackShape{experts, N, C, 0}, group, *out, (cudaStream_t)stream);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -300,8 +334,8 @@ int moe_w4_unpack(int32_t dtype, int32_t experts, int32_t N, int32_t C, int32_t 
   if (rc != MOE_OK) return rc;
   if (!d_out) return MOE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(d_out) & 15) return MOE_ERR_ALIGN;
-  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_unpack<float>(*w, experts, N, C, group, d_out, (cudaStream_t)stream)
-                                          : launch_unpack<__nv_bfloat16>(*w, experts, N, C, group, d_out, (cudaStream_t)stream);
+  cudaError_t e = dtype == MOE_DTYPE_FP32 ? launch_unpack<float>(*w, PackShape{experts, N, C, 0}, group, d_out, (cudaStream_t)stream)
+                                          : launch_unpack<__nv_bfloat16>(*w, PackShape{experts, N, C, 0}, group, d_out, (cudaStream_t)stream);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
@@ -312,7 +346,7 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
   if (M < 0) return MOE_ERR_ARG;
   if (M == 0) return MOE_OK;
   if (!d_x || !d_y || (experts > 1 && !d_expert)) return MOE_ERR_ARG;
-  if (experts > 65535 || C > (1 << 25)) return MOE_ERR_UNSUPPORTED;  // (16-bit matrix numbers, 32-bit offsets into a batch of x)
+  if (experts > 65535) return MOE_ERR_UNSUPPORTED;  // (matrix numbers are held in 16 bits)
   if (((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) & 15) || (reinterpret_cast<uintptr_t>(d_expert) & 3))
     return MOE_ERR_ALIGN;
   const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, M};
