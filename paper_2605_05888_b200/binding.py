@@ -6,7 +6,6 @@ missing or no CUDA device is present, calls raise.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -149,8 +148,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:  # (the stream object that torch.cuda.current_stream() makes costs as much as a launch)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -211,9 +210,13 @@ def moe_combine_ep(cfg: MoeConfig, staging, rows_back, cap_rows: int, out_rows, 
                                 _ptr(status), _stream(stream)), "moe_combine_ep")
 
 
-def _on_device_of(t: torch.Tensor):
-    """The calls that take no plan run on the current device: make it the tensors' one."""
-    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+def _call_on(t: torch.Tensor, where: str, stream, fn, *args) -> None:
+    """A call that takes no plan runs on the current device: it is made the tensors' one."""
+    if t.device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)), where)
+    else:
+        with torch.cuda.device(t.device):
+            _check(fn(*args, _stream(stream)), where)
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -234,24 +237,21 @@ def moe_w4_matvec(w: W4, x, expert, y, stream=None) -> None:
         raise ValueError(f"x {x.dtype} {tuple(x.shape)} and y {y.dtype} {tuple(y.shape)} for matrices [{w.N}, {w.C}]")
     if expert is not None and (expert.dtype != torch.int32 or expert.shape != (M,)):
         raise ValueError("expert is int32 [M]")
-    with _on_device_of(w.codes):
-        _check(lib().moe_w4_matvec(w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y), _stream(stream)), "moe_w4_matvec")
+    _call_on(w.codes, "moe_w4_matvec", stream, lib().moe_w4_matvec, w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y))
 
 
 def moe_w4_pack(weights, out: W4, stream=None) -> None:
     """bf16 or fp32 weights [experts, N, C] into out's 4-bit codes and scales."""
     _w4_shape(out, weights)
     dtype = _dtype_code(weights)
-    with _on_device_of(out.codes):
-        _check(lib().moe_w4_pack(dtype, out.experts, out.N, out.C, out.group, _ptr(weights), out.ref, _stream(stream)), "moe_w4_pack")
+    _call_on(out.codes, "moe_w4_pack", stream, lib().moe_w4_pack, dtype, out.experts, out.N, out.C, out.group, _ptr(weights), out.ref)
 
 
 def moe_w4_unpack(w: W4, out, stream=None) -> None:
     """The weights that w's codes stand for, into out [experts, N, C] (bf16 or fp32)."""
     _w4_shape(w, out)
     dtype = _dtype_code(out)
-    with _on_device_of(w.codes):
-        _check(lib().moe_w4_unpack(dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out), _stream(stream)), "moe_w4_unpack")
+    _call_on(w.codes, "moe_w4_unpack", stream, lib().moe_w4_unpack, dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out))
 
 
 class Plan:

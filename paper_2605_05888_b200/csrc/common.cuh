@@ -46,7 +46,7 @@ struct Scratch {          // device pointers carved out of the caller's workspac
   float* route_logits;    // [T, 256] router logits, more than 64 experts: the chain kernel's, or the tensor-core filter's approximate ones
   int route_slices;       // the slices of h that they are in (route_direct_kernel's: [route_slices, T, 256]); 0: another router
   float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens; else nullptr)
-  unsigned* few_sync;     // [4]   and its two grid barriers (left as they were found by every launch)
+  unsigned* few_sync;     // [64]  and its two grid barriers (every launch flips their highest bits)
   float* route_wnorm2;    // [256]    squared norms of the router's weight rows, recomputed by every call (filter)
   // moe_layer's internal buffers
   int* topk_idx;

@@ -32,7 +32,7 @@ struct LayerFewParams {
   int slices, slice_cols;  // of the router's sums
   float* logits;           // [slices, T, E]
   void* inter;             // [entries, 8, F]: the gate / up results of an entry's tokens
-  unsigned* sync;          // two barriers: {arrived, generation} each
+  unsigned* sync;          // two barriers' counters, 128 bytes apart
   int* topk_idx;           // the picks and rows per expert, as moe_layer leaves them (every TP shard listed)
   float* topk_w;
   int* expert_count;
@@ -40,29 +40,25 @@ struct LayerFewParams {
   unsigned long long wait_ns;
 };
 
-// Every CTA of the grid arrives exactly once per launch and barrier, also one whose wait ran out before, so the counters are
-// left as they were found whatever happens.  Everything written before is visible behind it (to loads that miss L1).
+// Every CTA of the grid arrives exactly once per launch and barrier, also one whose wait ran out before: together they add 2^31, so
+// that the counter's highest bit flips with the last one and what is below it is as it was.  What was written before is visible
+// behind it (to loads that miss L1).
 __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which) {
   __syncthreads();
   if (threadIdx.x == 0) {
-    unsigned* arrived = p.sync + 2 * which;
-    int* generation = reinterpret_cast<int*>(p.sync + 2 * which + 1);
-    const int before = ld_acquire(generation);
-    __threadfence();
-    if (atomicAdd(arrived, 1u) == gridDim.x - 1) {
-      atomicExch(arrived, 0u);
-      __threadfence();
-      st_release(generation, before + 1);
-    } else {
-      const unsigned long long t0 = globaltimer();
-      while (ld_acquire(generation) == before) {
-        if (globaltimer() - t0 > p.wait_ns) {
-          set_status(p.status, MOE_ERR_TIMEOUT, kWaitGrid);
-          break;
-        }
+    unsigned* arrived = p.sync + 32 * which;
+    const unsigned mine = blockIdx.x == 0 ? 0x80000000u - (gridDim.x - 1) : 1u;
+    unsigned before;
+    asm volatile("atom.add.release.gpu.global.u32 %0, [%1], %2;" : "=r"(before) : "l"(arrived), "r"(mine) : "memory");
+    unsigned long long t0 = 0;
+    while (!((before ^ (unsigned)ld_acquire(reinterpret_cast<int*>(arrived))) >> 31)) {
+      const unsigned long long now = globaltimer();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > p.wait_ns) {
+        set_status(p.status, MOE_ERR_TIMEOUT, kWaitGrid);
+        break;
       }
     }
-    __threadfence();
   }
   __syncthreads();
 }
@@ -75,106 +71,184 @@ struct LfShared {
   unsigned char count[kLfEntries];
   unsigned char token[kLfEntries * kLfSlots];       // its tokens
   unsigned char pick[kLfEntries * kLfSlots];        // and which of a token's picks it is
-  int warp_used[kMaxExperts / 32];
 };
-struct LfSelect {  // where the rows are streamed through later
-  float red[kLfMaxWarps][kLfTokens];
+constexpr int kLfBatch = 2;  // experts that a CTA scores at a time
+struct LfSelect {            // where the rows are streamed through later
+  float red[kLfMaxWarps][kLfBatch * kLfTokens];
   int idx[kLfTokens * kLfPicks];
-  unsigned mask[kMaxExperts];
-  int pos[kMaxExperts];  // a used expert's first entry
-  float logits[kLfTokens * kMaxExperts];
+  unsigned mask[kMaxExperts];            // the tokens that picked an expert
+  unsigned used[kMaxExperts / 32];       // bit per expert: picked at all,
+  unsigned many[kMaxExperts / 32];       // by more than kLfSlots tokens
 };
 
-// The logits (or a slice's part of them): a CTA per expert and slice, columns over its threads.
-template <typename T>
+template <int N>
+__device__ __forceinline__ float lf_dot(const uint4& x, const uint4& w);
+template <>
+__device__ __forceinline__ float lf_dot<4>(const uint4& x, const uint4& w) {
+  float a[4], b[4], s = 0.0f;
+  Vec16<float>::unpack(x, a);
+  Vec16<float>::unpack(w, b);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s = __fmaf_rn(a[j], b[j], s);
+  return s;
+}
+template <>
+__device__ __forceinline__ float lf_dot<8>(const uint4& x, const uint4& w) {
+  const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {w.x, w.y, w.z, w.w};
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s = fma_bf16_hi(a[j], b[j], fma_bf16_lo(a[j], b[j], s));
+  return s;
+}
+
+// The logits (or a slice's part of them): a CTA takes kLfBatch experts of a slice, columns over its threads.  TT: tokens at most.
+template <typename T, int TT>
 __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) {
-  constexpr int N = Vec16<T>::N;
+  constexpr int N = Vec16<T>::N, SUMS = kLfBatch * TT;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (int task = blockIdx.x; task < p.E * p.slices; task += gridDim.x) {
-    const int e = task / p.slices, slice = task % p.slices;
+  const int batches = (p.E + kLfBatch - 1) / kLfBatch;
+  for (int task = blockIdx.x; task < batches * p.slices; task += gridDim.x) {
+    const int slice = task / batches, e0 = (task - slice * batches) * kLfBatch;
     const int c0 = slice * p.slice_cols, c1 = min(p.H, c0 + p.slice_cols);
-    float acc[kLfTokens] = {};
+    float acc[SUMS] = {};
     for (int c = c0 + (int)threadIdx.x * N; c < c1; c += blockDim.x * N) {
-      float w[N];
-      Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)e * p.H + c), w);
+      uint4 w[kLfBatch];
 #pragma unroll
-      for (int t = 0; t < kLfTokens; ++t) {
+      for (int i = 0; i < kLfBatch; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)min(e0 + i, p.E - 1) * p.H + c));
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
         if (t >= p.T) break;
-        float v[N], part = 0.0f;
-        Vec16<T>::unpack(*reinterpret_cast<const uint4*>((const T*)p.x + (size_t)t * p.H + c), v);
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>((const T*)p.x + (size_t)t * p.H + c));
 #pragma unroll
-        for (int j = 0; j < N; ++j) part = __fmaf_rn(v[j], w[j], part);
-        acc[t] += part;
+        for (int i = 0; i < kLfBatch; ++i) acc[i * TT + t] += lf_dot<N>(x, w[i]);
       }
     }
+    // Sums over the lanes: each step halves the values a lane holds, so that SUMS of them take SUMS - 1 exchanges.
+    int mine = 0;
 #pragma unroll
-    for (int t = 0; t < kLfTokens; ++t) {
-      if (t >= p.T) break;
-      const float sum = group_sum<32>(acc[t]);
-      if (lane == 0) s.red[warp][t] = sum;
+    for (int step = 0; step < 5; ++step) {
+      const int off = 16 >> step, n = (SUMS / 2) >> step;
+      if (n >= 1) {
+        const bool upper = lane & off;
+#pragma unroll
+        for (int j = 0; j < SUMS / 2; ++j) {
+          if (j >= n) break;
+          const float keep = upper ? acc[j + n] : acc[j], give = upper ? acc[j] : acc[j + n];
+          acc[j] = keep + __shfl_xor_sync(0xffffffffu, give, off);
+        }
+        mine += upper ? n : 0;
+      } else {
+        acc[0] += __shfl_xor_sync(0xffffffffu, acc[0], off);
+      }
     }
+    if (lane % (32 / SUMS) == 0) s.red[warp][mine] = acc[0];
     __syncthreads();
-    if ((int)threadIdx.x < p.T) {
+    if ((int)threadIdx.x < SUMS) {
       float sum = 0.0f;
-#pragma unroll
       for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += s.red[i][threadIdx.x];
-      __stcg(p.logits + ((size_t)slice * p.T + threadIdx.x) * p.E + e, sum);
+      const int e = e0 + (int)threadIdx.x / TT, t = threadIdx.x % TT;
+      if (e < p.E && t < p.T) __stcg(p.logits + ((size_t)slice * p.T + t) * p.E + e, sum);
     }
     __syncthreads();
   }
 }
 
-// Every CTA selects for itself; returns the number of entries.
-__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  for (int i = tid; i < p.T * p.E; i += blockDim.x) {
-    float sum = 0.0f;
-    for (int j = 0; j < p.slices; ++j) sum += __ldcg(p.logits + (size_t)j * p.T * p.E + i);
-    q.logits[i] = p.bias != nullptr ? sum + p.bias[i % p.E] : sum;
+// A warp selects the picks of token t (as select_topk does, from registers).
+template <int NJ>
+__device__ __forceinline__ void lf_pick(const LayerFewParams& p, LfShared& s, LfSelect& q, int t) {
+  const int lane = threadIdx.x % 32;
+  float v[NJ] = {};
+  for (int i = 0; i < p.slices; ++i)
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      if (lane + 32 * j < p.E) v[j] += __ldcg(p.logits + ((size_t)i * p.T + t) * p.E + lane + 32 * j);
+  unsigned key[NJ];  // 0: no expert, or picked already
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int e = lane + 32 * j;
+    if (p.bias != nullptr && e < p.E) v[j] += __ldg(p.bias + e);
+    key[j] = e < p.E ? max(order_key(v[j]), 1u) : 0u;
   }
-  if (tid < kMaxExperts) q.mask[tid] = 0;
-  __syncthreads();
-  if (p.E <= 64) select_topk<32, 2>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
-  else select_topk<32, 8>(q.logits, p.E, p.T, 0, p.E, p.K, p.renorm, q.idx, s.w, nullptr, 1);
-  __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
-    atomicOr(&q.mask[q.idx[a]], 1u << (a / p.K));
+  unsigned my_key = 0, first_key = 0;
+  int my_e = 0;
+  for (int k = 0; k < p.K; ++k) {
+    unsigned best = key[0];
+#pragma unroll
+    for (int j = 1; j < NJ; ++j) best = max(best, key[j]);
+    best = __reduce_max_sync(0xffffffffu, best);
+    unsigned e = 0xffffffffu;
+#pragma unroll
+    for (int j = NJ - 1; j >= 0; --j)
+      if (key[j] == best) e = (unsigned)(lane + 32 * j);
+    e = __reduce_min_sync(0xffffffffu, e);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+      if (e == (unsigned)(lane + 32 * j)) key[j] = 0u;
+    if (k == 0) first_key = best;
+    if (lane == k) { my_e = (int)e; my_key = best; }
+  }
+  auto value = [](unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); };
+  const float m = value(first_key);
+  float z = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+    if (lane + 32 * j < p.E) z += expf(v[j] - m);
+  z = group_sum<32>(z);
+  float w = lane < p.K ? expf(value(my_key) - m) / z : 0.0f;
+  if (p.renorm) w = w / group_sum<32>(w);
+  if (lane < p.K) {
+    s.w[t * p.K + lane] = w;
+    q.idx[t * p.K + lane] = my_e;
+    atomicOr(&q.mask[my_e], 1u << t);
+    atomicOr(&q.used[my_e / 32], 1u << (my_e % 32));
     if (blockIdx.x == 0)
       for (int sh = 0; sh < p.tp; ++sh) {
-        p.topk_idx[a * p.tp + sh] = q.idx[a] * p.tp + sh;
-        p.topk_w[a * p.tp + sh] = s.w[a];
+        p.topk_idx[(t * p.K + lane) * p.tp + sh] = my_e * p.tp + sh;
+        p.topk_w[(t * p.K + lane) * p.tp + sh] = w;
       }
   }
+}
+
+// Before the barrier.
+__device__ __forceinline__ void lf_clear(LfSelect& q) {
+  if (threadIdx.x < kMaxExperts) q.mask[threadIdx.x] = 0;
+  if (threadIdx.x < kMaxExperts / 32) q.used[threadIdx.x] = q.many[threadIdx.x] = 0;
+}
+
+// Every CTA selects for itself; returns the number of entries: one per used expert and kLfSlots tokens of it.
+__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
+  const int tid = threadIdx.x;
+  for (int t = tid / 32; t < p.T; t += blockDim.x / 32) {
+    if (p.E <= 64) lf_pick<2>(p, s, q, t);
+    else lf_pick<8>(p, s, q, t);
+  }
   __syncthreads();
+  if (p.T > kLfSlots) {
+    if (tid < kMaxExperts && __popc(q.mask[tid]) > kLfSlots) atomicOr(&q.many[tid / 32], 1u << (tid % 32));
+    __syncthreads();
+  }
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxExperts / 32; ++i) n += __popc(q.used[i]) + __popc(q.many[i]);
+  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
+    const int t = a / p.K, e = q.idx[a];
+    int at = 0;  // entries of the experts before e
+#pragma unroll
+    for (int i = 0; i < kMaxExperts / 32; ++i) {
+      const unsigned below = i < e / 32 ? 0xffffffffu : i == e / 32 ? (1u << (e % 32)) - 1u : 0u;
+      at += __popc(q.used[i] & below) + __popc(q.many[i] & below);
+    }
+    const int rank = __popc(q.mask[e] & ((1u << t) - 1u));
+    at += rank / kLfSlots;
+    s.token[at * kLfSlots + rank % kLfSlots] = (unsigned char)t;
+    s.pick[at * kLfSlots + rank % kLfSlots] = (unsigned char)(a - t * p.K);
+    if (rank % kLfSlots == 0) {
+      s.used[at] = (unsigned short)e;
+      s.count[at] = (unsigned char)min(kLfSlots, __popc(q.mask[e]) - rank);
+    }
+  }
   if (blockIdx.x == 0)
     for (int e = tid; e < p.E * p.tp; e += blockDim.x) p.expert_count[e] = __popc(q.mask[e / p.tp]);
-  // entries: one per used expert and eight tokens of it
-  const int tokens = tid < kMaxExperts ? __popc(q.mask[tid]) : 0, entries = (tokens + kLfSlots - 1) / kLfSlots;
-  int upto = entries;
-#pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, upto, off);
-    if (lane >= off) upto += v;
-  }
-  if (lane == 31 && tid < kMaxExperts) s.warp_used[warp] = upto;
-  __syncthreads();
-  int pos = upto - entries, n = 0;
-#pragma unroll
-  for (int i = 0; i < kMaxExperts / 32; ++i) {
-    if (i < warp) pos += s.warp_used[i];
-    n += s.warp_used[i];
-  }
-  if (tid < kMaxExperts) q.pos[tid] = pos;
-  for (int i = 0; i < entries; ++i) {
-    s.used[pos + i] = (unsigned short)tid;
-    s.count[pos + i] = (unsigned char)min(kLfSlots, tokens - i * kLfSlots);
-  }
-  __syncthreads();
-  for (int a = tid; a < p.T * p.K; a += blockDim.x) {
-    const int t = a / p.K, e = q.idx[a], slot = q.pos[e] * kLfSlots + __popc(q.mask[e] & ((1u << t) - 1u));
-    s.token[slot] = (unsigned char)t;
-    s.pick[slot] = (unsigned char)(a % p.K);
-  }
   __syncthreads();
   return n;
 }
@@ -194,7 +268,10 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
   const int lane = threadIdx.x % 32;
   if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
-  lf_router<X>(p, q);
+  if (p.T <= 1) lf_router<X, 1>(p, q);
+  else if (p.T <= 4) lf_router<X, 4>(p, q);
+  else lf_router<X, kLfTokens>(p, q);
+  lf_clear(q);
   grid_barrier(p, 0);
   const RsList list{s.used, s.count, s.token, lf_select(p, s, q)};
 
@@ -223,14 +300,15 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   __syncthreads();
   up.join(slots, finish_up);
   grid_barrier(p, 1);
+  auto store = [&](int row, int t, float v) { ((X*)p.y)[(size_t)t * p.H + row] = from_float<X>(v); };
   auto finish_down = [&](int, int row, int n0, int n1, const float* sums) {
-    const int r = lane % kRsRun, first = lane < kRsRun ? row : row + n0;
+    const int r = lane % kRsRun;
     if (r < (lane < kRsRun ? n0 : n1))
-      for (int t = 0; t < p.T; ++t) ((X*)p.y)[(size_t)t * p.H + first + r] = from_float<X>(sums[Down::sum_at(t, lane)]);
+      for (int t = 0; t < p.T; ++t) store(row + (lane < kRsRun ? 0 : n0) + r, t, sums[Down::sum_at(t, lane)]);
   };
   down.run(&start, slots, [&](int u, int slot) { return s.w[s.token[u * kLfSlots + slot] * p.K + s.pick[u * kLfSlots + slot]]; }, finish_down);
   __syncthreads();
-  down.join(slots, finish_down);
+  down.join_sums(slots, p.T, store);
 }
 
 template <typename W>
@@ -262,7 +340,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   if (device != p->device) return MOE_ERR_ARG;
   // the tokens' rows, and the gate / up results of at most two entries per expert, have 32-bit offsets
   const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
-  if (c.T * c.H * eb >= 1ll << 32 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 32) return MOE_ERR_UNSUPPORTED;
+  if (c.T * c.H * eb >= 1ll << 32 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 32 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
   LayerFewParams q = {};
   q.x = x;
   q.wr = wr;
@@ -279,7 +357,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.renorm = c.renormalize;
   q.tp = p->tp;
   // about a task per CTA, no slice under 256 columns; the scratch holds 256 sums per token
-  q.slices = max(1, min(min(p->sm_count, 256) / q.E, min(16, c.H / 256)));
+  q.slices = max(1, min(min(p->sm_count * kLfBatch, 256) / q.E, min(16, c.H / 256)));
   const int unit = 8;
   q.slice_cols = ((c.H + q.slices - 1) / q.slices + unit - 1) / unit * unit;
   q.slices = (c.H + q.slice_cols - 1) / q.slice_cols;

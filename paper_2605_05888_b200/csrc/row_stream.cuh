@@ -97,39 +97,52 @@ struct RsList {
   int n;
 };
 
-// The rows of one CTA: [begin, end) of `used` entries' rows laid end to end.  RT: rows of a tile.
+// n things in `parts` shares that differ by one at most: where share i begins and how many it has.  (32 bits and one division: the
+// kernels' latencies are made of such.)
+struct RsShare {
+  int begin, count;
+  __device__ __forceinline__ RsShare(unsigned n, unsigned parts, unsigned i) {
+    const unsigned each = n / parts, more = n - each * parts;
+    begin = (int)(each * i + min(i, more));
+    count = (int)(each + (i < more ? 1 : 0));
+  }
+};
+
+// The rows of one CTA: its share of `used` entries' rows laid end to end (fewer than 2^31).  RT: rows of a tile.
 struct RsRange {
-  long long begin, end;
-  int N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
+  int end, N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
   __device__ __forceinline__ RsRange(int used, int N_, int RT_) : N(N_), RT(RT_) {
-    const long long rows = (long long)used * N;
-    begin = rows * blockIdx.x / gridDim.x;
-    end = rows * (blockIdx.x + 1) / gridDim.x;
-    if (end <= begin) { tiles = 0; return; }
-    first_u = (int)(begin / N);
-    first_row = (int)(begin - (long long)first_u * N);
-    first_len = (int)min(end - begin, (long long)(N - first_row));
+    const RsShare mine((unsigned)(used * N), gridDim.x, blockIdx.x);
+    tiles = 0;
+    if (mine.count == 0) return;
+    end = mine.begin + mine.count;
+    first_u = (unsigned)mine.begin / (unsigned)N;
+    first_row = mine.begin - first_u * N;
+    first_len = min(mine.count, N - first_row);
     first_tiles = (first_len + RT - 1) / RT;
     full_tiles = (N + RT - 1) / RT;
-    const int last_u = (int)((end - 1) / N);
     tiles = first_tiles;
-    if (last_u > first_u) tiles += (last_u - first_u - 1) * full_tiles + (int)(end - (long long)last_u * N + RT - 1) / RT;
+    const int rest = mine.count - first_len;
+    if (rest > 0) {
+      const int whole = (unsigned)rest / (unsigned)N;
+      tiles += whole * full_tiles + (rest - whole * N + RT - 1) / RT;
+    }
   }
-  // matrix, first row and number of rows of tile i
+  // entry, first row and number of rows of tile i
   __device__ __forceinline__ void tile(int i, int& u, int& row, int& n) const {
     int start = first_row, len = first_len, count = first_tiles, k = i;
     u = first_u;
     if (i >= first_tiles) {
-      const int j = i - first_tiles, skip = j / full_tiles;
+      const int j = i - first_tiles, skip = (unsigned)j / (unsigned)full_tiles;
       u += 1 + skip;
       k = j - skip * full_tiles;
       start = 0;
-      len = (int)min((long long)N, end - (long long)u * N);
+      len = min(N, end - u * N);
       count = (len + RT - 1) / RT;
     }
-    row = (int)((long long)len * k / count);
-    n = (int)((long long)len * (k + 1) / count) - row;
-    row += start;
+    const RsShare rows(len, count, k);
+    row = start + rows.begin;
+    n = rows.count;
   }
 };
 
@@ -170,19 +183,19 @@ struct RowStream {
     lane = threadIdx.x % 32;
     chunks = (op.C + F::COLS - 1) / F::COLS;
     per_tile = KIND == kRsSum ? chunks * list.n : chunks;
-    const long long units = (long long)range.tiles * per_tile;
-    const int warp = threadIdx.x / 32;
-    const long long unit = units * warp / WARPS;
-    total = left = (int)(units * (warp + 1) / WARPS - unit);
+    const RsShare mine = share(threadIdx.x / 32);
+    total = left = mine.count;
     if (left > 0) {
-      tile_i = (int)(unit / per_tile);
-      const int c = (int)(unit - (long long)tile_i * per_tile);
+      tile_i = (unsigned)mine.begin / (unsigned)per_tile;
+      const int c = mine.begin - tile_i * per_tile;
       set_tile(tile_i, u, row, n0, n1);
-      if (KIND == kRsSum) u = c / chunks;
+      if (KIND == kRsSum) u = (unsigned)c / (unsigned)chunks;
       chunk = KIND == kRsSum ? c - u * chunks : c;
       set_pointers();
     }
   }
+
+  __device__ __forceinline__ RsShare share(int warp) const { return RsShare(range.tiles * per_tile, WARPS, warp); }  // units
 
   __device__ __forceinline__ void set_tile(int i, int& tu, int& trow, int& tn0, int& tn1) const {
     int n;
@@ -586,27 +599,44 @@ struct RowStream {
     }
   }
 
-  // Behind the barrier: the warp that a cut tile begins in adds what the following warps left, and finishes it.
+  // Behind the barrier: what the warps hold of cut tiles is added up in the warps' order and finished.
+  // kRsPairs, kRsRows: by the warp that the tile begins in, by finish as above.
   template <typename Finish>
   __device__ __forceinline__ void join(float* slots, Finish finish) {
     if (!pending) return;
-    const long long units = (long long)range.tiles * per_tile, tile_end = (long long)(m_tile + 1) * per_tile;
-    float* slot = slots + threadIdx.x / 32 * Z::SLOT;
+    const int tile_end = (m_tile + 1) * per_tile;
     for (int w = threadIdx.x / 32 + 1; w < WARPS; ++w) {
-      const long long begin = units * w / WARPS;
-      if (begin >= tile_end) break;
-      if (units * (w + 1) / WARPS == begin) continue;
-      if (KIND == kRsSum) {
-        const float* area = held_area(w);
+      const RsShare s = share(w);
+      if (s.begin >= tile_end) break;
+      if (s.count == 0) continue;
 #pragma unroll
-        for (int j = 0; j < Z::SLOT / 32; ++j) slot[j * 32 + lane] += area[j * 32 + lane];
-      } else {
-#pragma unroll
-        for (int j = 0; j < REGS; ++j) acc[j] += slots[w * Z::SLOT + j * 32 + lane];
+      for (int j = 0; j < REGS; ++j) acc[j] += slots[w * Z::SLOT + j * 32 + lane];
+    }
+    finish(m_u, m_row, m_n0, m_n1, slots);
+  }
+  // kRsSum: by all threads, a value each; store(row of y, token, value).
+  template <typename Store>
+  __device__ __forceinline__ void join_sums(const float* slots, int tokens, Store store) {
+    for (int i = 0; i < range.tiles; ++i) {
+      const int lo = i * per_tile, hi = lo + per_tile;
+      int tu, row0, m0, m1;
+      set_tile(i, tu, row0, m0, m1);
+      for (int at = threadIdx.x; at < tokens * kRsTile; at += Z::THREADS) {
+        const int t = at / kRsTile, r = at % kRsTile;
+        float v = 0.0f;
+        bool whole = false;
+#pragma unroll 4
+        for (int w = 0; w < WARPS; ++w) {
+          const RsShare s = share(w);
+          const int s_end = s.begin + s.count;
+          if (s.count == 0 || s_end <= lo || s.begin >= hi) continue;
+          whole = s.begin <= lo && s_end >= hi;  // (finished by its warp)
+          v += (s.begin > lo ? held_area(w) : slots + w * Z::SLOT)[sum_at(t, r)];
+        }
+        const int k = r % kRsRun;
+        if (!whole && k < (r < kRsRun ? m0 : m1)) store(row0 + (r < kRsRun ? 0 : m0) + k, t, v);
       }
     }
-    __syncwarp();
-    finish(m_u, m_row, m_n0, m_n1, slot);
   }
   // kRsSum: warp w's sums of a tile that began before its share, in its ring.
   __device__ __forceinline__ float* held_area(int w) const {
