@@ -115,12 +115,16 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
       uint4 w[kLfBatch];
 #pragma unroll
       for (int i = 0; i < kLfBatch; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>((const T*)p.wr + (size_t)min(e0 + i, p.E - 1) * p.H + c));
+      constexpr int TG = TT < 8 ? TT : 8;  // tokens whose loads are in flight together (past the last one: the last one's again)
 #pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        if (t >= p.T) break;
-        const uint4 x = __ldg(reinterpret_cast<const uint4*>((const T*)p.x + (size_t)t * p.H + c));
+      for (int t0 = 0; t0 < TT; t0 += TG) {
+        uint4 x[TG];
 #pragma unroll
-        for (int i = 0; i < kLfBatch; ++i) acc[i * TT + t] += lf_dot<N>(x, w[i]);
+        for (int t = 0; t < TG; ++t) x[t] = __ldg(reinterpret_cast<const uint4*>((const T*)p.x + (size_t)min(t0 + t, p.T - 1) * p.H + c));
+#pragma unroll
+        for (int t = 0; t < TG; ++t)
+#pragma unroll
+          for (int i = 0; i < kLfBatch; ++i) acc[i * TT + t0 + t] += lf_dot<N>(x[t], w[i]);
       }
     }
     // Sums over the lanes: each step halves the values a lane holds, so that SUMS of them take SUMS - 1 exchanges.
@@ -157,16 +161,26 @@ __device__ __forceinline__ void lf_router(const LayerFewParams& p, LfSelect& s) 
 template <int NJ>
 __device__ __forceinline__ void lf_pick(const LayerFewParams& p, LfShared& s, LfSelect& q, int t) {
   const int lane = threadIdx.x % 32;
-  float v[NJ] = {};
-  for (int i = 0; i < p.slices; ++i)
+  float v[NJ] = {}, b[NJ];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
-      if (lane + 32 * j < p.E) v[j] += __ldcg(p.logits + ((size_t)i * p.T + t) * p.E + lane + 32 * j);
+  for (int j = 0; j < NJ; ++j) b[j] = p.bias != nullptr && lane + 32 * j < p.E ? __ldg(p.bias + lane + 32 * j) : 0.0f;
+  const float* from = p.logits + t * p.E + lane;
+  for (int i0 = 0; i0 < p.slices; i0 += 4) {  // four slices' loads in flight
+    float l[4][NJ];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) l[i][j] = i0 + i < p.slices && lane + 32 * j < p.E ? __ldcg(from + (i0 + i) * p.T * p.E + 32 * j) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) v[j] += l[i][j];
+  }
   unsigned key[NJ];  // 0: no expert, or picked already
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     const int e = lane + 32 * j;
-    if (p.bias != nullptr && e < p.E) v[j] += __ldg(p.bias + e);
+    v[j] += b[j];
     key[j] = e < p.E ? max(order_key(v[j]), 1u) : 0u;
   }
   unsigned my_key = 0, first_key = 0;
@@ -270,6 +284,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
   if (p.T <= 1) lf_router<X, 1>(p, q);
   else if (p.T <= 4) lf_router<X, 4>(p, q);
+  else if (p.T <= 8) lf_router<X, 8>(p, q);
   else lf_router<X, kLfTokens>(p, q);
   lf_clear(q);
   grid_barrier(p, 0);
@@ -285,7 +300,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
       if (Up::kMma && j % 4 >= 2) continue;
       const float upper = Up::kMma ? up.acc[Up::kMma ? j + 2 : j] : __shfl_down_sync(0xffffffffu, up.acc[j], kRsRun);
       const int t = up.token(j), f = up.row_of(j);
-      if (t < s.count[u] && f < n0 && (Up::kMma || lane < kRsRun))
+      if (t < s.count[u] && f < n0 && (Up::kMma || (lane < kRsRun && up.is_first())))
         ((X*)p.inter)[((size_t)u * kLfSlots + t) * p.F + row + f] = from_float<X>(lf_silu_mul(up.acc[j], upper));
     }
   };

@@ -323,22 +323,24 @@ struct RowStream {
     }
   }
 
-  // A stage's products added to acc.  MT: 1 where the runs have at most 8 rows, else 2.  (Slots without a token hold anything: their
+  // A stage's products added to acc.  MT (tensor cores): 1 where the runs have at most 8 rows, else 2.  (Slots without a token hold anything: their
   // sums are not read.)
   template <int MT>
   __device__ __forceinline__ void multiply(uint32_t a, int tokens) {
     if constexpr (!kMma) {
-      float w[32];
+      // MT 1, 2, 4: that many lanes share a row (of 16, 8, 4 per run), each with its part of the columns.
+      constexpr int UNITS = 8 / MT;
+      float w[4 * UNITS];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + place(lane, c)), w + 4 * c);
+      for (int c = 0; c < UNITS; ++c) Vec16<float>::unpack(lds128(a + place(lane / kRsRun * kRsRun + lane % kRsRun / MT, c * MT + lane % MT)), w + 4 * c);
 #pragma unroll
       for (int t = 0; t < SLOTS; ++t) {
         if (t >= tokens) break;
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
+        for (int c = 0; c < UNITS; ++c) {
           float v[4];
-          Vec16<float>::unpack(lds128(a + Z::A + place(t, c)), v);
+          Vec16<float>::unpack(lds128(a + Z::A + place(t, c * MT + lane % MT)), v);
           s0 = __fmaf_rn(w[4 * c], v[0], s0);
           s1 = __fmaf_rn(w[4 * c + 1], v[1], s1);
           s0 = __fmaf_rn(w[4 * c + 2], v[2], s0);
@@ -534,8 +536,14 @@ struct RowStream {
       } else {
         copies_wait<Z::STAGES - 1>();
         __syncwarp();
-        if (m_n0 > 8) multiply<2>(stage, m_tokens);
-        else multiply<1>(stage, m_tokens);
+        if constexpr (kMma) {
+          if (m_n0 > 8) multiply<2>(stage, m_tokens);
+          else multiply<1>(stage, m_tokens);
+        } else {
+          if (m_n0 > 8) multiply<1>(stage, m_tokens);
+          else if (m_n0 > 4) multiply<2>(stage, m_tokens);
+          else multiply<4>(stage, m_tokens);
+        }
       }
       next = stage;
       stage = stage + Z::STAGE == ring + Z::STAGES * Z::STAGE ? ring : stage + Z::STAGE;
@@ -543,11 +551,18 @@ struct RowStream {
       const bool last = i + 1 == total;
       if (m_chunk < chunks && !last) continue;
       // the end of a matrix's columns, or of the share
+      if constexpr (!kMma) {
+#pragma unroll
+        for (int j = 0; j < REGS; ++j) {
+          if (row_lanes() >= 2) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 1);
+          if (row_lanes() >= 4) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);
+        }
+      }
       if (KIND == kRsSum) {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
           const int t = token(j);
-          if (t < m_tokens) {
+          if (t < m_tokens && is_first()) {
             float* to = slot + sum_at(list.token[m_u * SLOTS + t], run_of(j) * kRsRun + row_of(j));
             *to = __fmaf_rn(weight(m_u, t), acc[j], *to);
           }
@@ -646,7 +661,10 @@ struct RowStream {
   // Of sum number j: the token's slot, the run, the row in it.
   __device__ __forceinline__ int token(int j) const { return kMma ? j / 4 % NT * 8 + lane % 4 * 2 + j % 2 : j; }
   __device__ __forceinline__ int run_of(int j) const { return kMma ? j / 2 % 2 : lane / kRsRun; }
-  __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun; }
+  __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun / row_lanes(); }
+  // fp32: how many lanes hold a row's sums, and the first of them.
+  __device__ __forceinline__ int row_lanes() const { return m_n0 > 8 ? 1 : m_n0 > 4 ? 2 : 4; }
+  __device__ __forceinline__ bool is_first() const { return kMma || lane % row_lanes() == 0; }
 };
 
 }  // namespace moehub
