@@ -138,7 +138,8 @@ size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, s
   t.route_wnorm2 = filter ? (float*)take(sizeof(float) * 256) : nullptr;
   if (!c.identity_experts && c.T > 0 && c.T <= MOE_FEW_MAX_TOKENS) {
     t.few_logits = (float*)take(sizeof(float) * 256 * (size_t)c.T);
-    t.few_sync = (unsigned*)take(sizeof(unsigned) * 64);
+    t.few_sync = (unsigned*)take(sizeof(unsigned) * 96);
+    t.few_partial = (float*)take(sizeof(float) * kFewPartial * (size_t)c.T);
   }
   t.topk_idx = (int*)take(sizeof(int) * (size_t)c.T * c.K);
   t.topk_w = (float*)take(sizeof(float) * (size_t)c.T * c.K);
@@ -224,7 +225,7 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
       cudaMemset(p->s.ord_exit, 0, sizeof(int) * 2) != cudaSuccess ||
       cudaMemset(p->s.gemm1_done, 0, sizeof(int) * (size_t)(g.P + 4)) != cudaSuccess ||
       cudaMemset(p->s.clock_probe, 0, 2 * sizeof(unsigned long long)) != cudaSuccess ||
-      (p->s.few_sync && cudaMemset(p->s.few_sync, 0, sizeof(unsigned) * 64) != cudaSuccess)) {
+      (p->s.few_sync && cudaMemset(p->s.few_sync, 0, sizeof(unsigned) * 96) != cudaSuccess)) {
     delete p;
     return MOE_ERR_CUDA;
   }

@@ -22,6 +22,7 @@ enum WaitSite { kWaitTileTable = 1, kWaitMbarTma = 3, kWaitMbarMma = 4,
                 kWaitMbarEpi = 5, kWaitMbarTmemFree = 6, kWaitTileReady = 7, kWaitItem = 8,
                 kWaitGrid = 9 };
 
+constexpr int kFewPartial = 16384;
 struct Scratch {          // device pointers carved out of the caller's workspace
   int* status;            // [4]
   int* pool_next;         // [1]   paged mode: next free tile
@@ -46,7 +47,8 @@ struct Scratch {          // device pointers carved out of the caller's workspac
   float* route_logits;    // [T, 256] router logits, more than 64 experts: the chain kernel's, or the tensor-core filter's approximate ones
   int route_slices;       // the slices of h that they are in (route_direct_kernel's: [route_slices, T, 256]); 0: another router
   float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens; else nullptr)
-  unsigned* few_sync;     // [64]  and its two grid barriers (every launch flips their highest bits)
+  unsigned* few_sync;     // [96]  its three grid barriers (every launch flips their highest bits)
+  float* few_partial;     // [kFewPartial, T] and its outputs in parts, where their rows are few (parts * H <= kFewPartial)
   float* route_wnorm2;    // [256]    squared norms of the router's weight rows, recomputed by every call (filter)
   // moe_layer's internal buffers
   int* topk_idx;

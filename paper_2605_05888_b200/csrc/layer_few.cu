@@ -32,7 +32,9 @@ struct LayerFewParams {
   int slices, slice_cols;  // of the router's sums
   float* logits;           // [slices, T, E]
   void* inter;             // [entries, 8, F]: the gate / up results of an entry's tokens
-  unsigned* sync;          // two barriers' counters, 128 bytes apart
+  unsigned* sync;          // three barriers' counters, 128 bytes apart
+  float* partial;          // [down_parts, T, H]: the outputs' parts, where there are several
+  int down_parts;
   int* topk_idx;           // the picks and rows per expert, as moe_layer leaves them (every TP shard listed)
   float* topk_w;
   int* expert_count;
@@ -291,7 +293,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   const RsList list{s.used, s.count, s.token, lf_select(p, s, q)};
 
   // gate and up rows of the used experts
-  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, p.F, p.H, p.E};
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, p.F, p.H, p.E, 1};
   typedef RowStream<W, 1, kRsPairs> Up;
   Up up(gate_up, list, ring);
   auto finish_up = [&](int u, int row, int n0, int, const float*) {
@@ -307,7 +309,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   up.run(nullptr, slots, [](int, int) { return 0.0f; }, finish_up);
 
   // the outputs; the first down rows are on their way while the other CTAs finish
-  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, p.H, p.F, p.E};
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, p.H, p.F, p.E, p.down_parts};
   typedef RowStream<W, 1, kRsSum> Down;
   Down down(down_op, list, ring);
   Down start = down;
@@ -315,7 +317,11 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   __syncthreads();
   up.join(slots, finish_up);
   grid_barrier(p, 1);
-  auto store = [&](int row, int t, float v) { ((X*)p.y)[(size_t)t * p.H + row] = from_float<X>(v); };
+  float* part = p.down_parts > 1 ? p.partial + (size_t)(blockIdx.x % p.down_parts) * p.T * p.H : nullptr;
+  auto store = [&](int row, int t, float v) {
+    if (part != nullptr) part[(size_t)t * p.H + row] = v;
+    else ((X*)p.y)[(size_t)t * p.H + row] = from_float<X>(v);
+  };
   auto finish_down = [&](int, int row, int n0, int n1, const float* sums) {
     const int r = lane % kRsRun;
     if (r < (lane < kRsRun ? n0 : n1))
@@ -324,6 +330,14 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   down.run(&start, slots, [&](int u, int slot) { return s.w[s.token[u * kLfSlots + slot] * p.K + s.pick[u * kLfSlots + slot]]; }, finish_down);
   __syncthreads();
   down.join_sums(slots, p.T, store);
+  if (p.down_parts > 1) {
+    grid_barrier(p, 2);
+    for (int i = blockIdx.x * Z::THREADS + threadIdx.x; i < p.T * p.H; i += gridDim.x * Z::THREADS) {
+      float v = 0.0f;
+      for (int j = 0; j < p.down_parts; ++j) v += __ldcg(p.partial + (size_t)j * p.T * p.H + i);
+      ((X*)p.y)[i] = from_float<X>(v);
+    }
+  }
 }
 
 template <typename W>
@@ -344,6 +358,19 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
 }
+// Where a CTA's share of the outputs is few rows, the loop over their columns is bound by its own latencies, not by bytes: several CTAs then share
+// more rows, each a part of the terms, and add up behind a third barrier, which costs about 2 us.  Measured, the down rows' part alone, us, one CTA / four
+// per range of rows: H 1024, F 2048, three tokens of 16 experts, bf16 7.7 / 3.2, fp32 14.6 / 7.4; F 4096, one token, fp32 9.9 / 4.5.
+static int down_parts(const moe_plan* p, int group) {
+  const moe_config_t& c = p->cfg;
+  const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
+  const double us = (double)min(c.T * p->route_K, p->route_E) * c.H * c.F * p->tp * bits / 8.0 / 6.0e6;  // of reading the down rows
+  int parts = 1;
+  while (parts < 16 && c.H * parts < 24 * p->sm_count) parts *= 2;
+  const double rows = (double)c.H / p->sm_count;
+  return us * (16.0 / rows - 1.0) > 4.0 ? parts : 1;
+}
+
 // The checks and the launch that both entry points share.
 static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bias, LfMatrix wg, LfMatrix wu, LfMatrix wd, int group,
                      void* y, cudaStream_t st) {
@@ -376,6 +403,8 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   const int unit = 8;
   q.slice_cols = ((c.H + q.slices - 1) / q.slices + unit - 1) / unit * unit;
   q.slices = (c.H + q.slice_cols - 1) / q.slice_cols;
+  q.down_parts = down_parts(p, group);
+  q.partial = p->s.few_partial;
   q.logits = p->s.few_logits;
   q.inter = p->s.inter;
   q.sync = p->s.few_sync;

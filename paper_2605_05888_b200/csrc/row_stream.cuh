@@ -87,6 +87,7 @@ struct RsOperand {
   const __nv_bfloat16* s1;
   const void* x;                // token rows [.., C]
   int N, C, matrices;           // matrices: all there are
+  int parts;                    // kRsSum: CTAs that share a range of rows, each a part of the sums' terms (1: none)
 };
 
 // What is to be multiplied: entries, each a matrix and the up to 8 * NT tokens that it is for (a matrix with more tokens has
@@ -109,11 +110,11 @@ struct RsShare {
   }
 };
 
-// The rows of one CTA: its share of `used` entries' rows laid end to end (fewer than 2^31).  RT: rows of a tile.
+// The rows of one CTA (or of `parts` CTAs): its share of `used` entries' rows laid end to end (fewer than 2^31).  RT: rows of a tile.
 struct RsRange {
   int end, N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
-  __device__ __forceinline__ RsRange(int used, int N_, int RT_) : N(N_), RT(RT_) {
-    const RsShare mine((unsigned)(used * N), gridDim.x, blockIdx.x);
+  __device__ __forceinline__ RsRange(int used, int N_, int RT_, unsigned group, unsigned groups) : N(N_), RT(RT_) {
+    const RsShare mine(group < groups ? (unsigned)(used * N) : 0u, groups, group);
     tiles = 0;
     if (mine.count == 0) return;
     end = mine.begin + mine.count;
@@ -180,7 +181,7 @@ struct RowStream {
   int lane;
 
   __device__ __forceinline__ RowStream(const RsOperand& op_, const RsList& list_, uint32_t ring_)
-      : op(op_), list(list_), range(KIND == kRsSum ? 1 : list_.n, op_.N, KIND == kRsPairs ? kRsRun : kRsTile), ring(ring_) {
+      : op(op_), list(list_), range(KIND == kRsSum ? 1 : list_.n, op_.N, KIND == kRsPairs ? kRsRun : kRsTile, blockIdx.x / op_.parts, gridDim.x / op_.parts), ring(ring_) {
     lane = threadIdx.x % 32;
     chunks = (op.C + F::COLS - 1) / F::COLS;
     per_tile = KIND == kRsSum ? chunks * list.n : chunks;
@@ -196,7 +197,10 @@ struct RowStream {
     }
   }
 
-  __device__ __forceinline__ RsShare share(int warp) const { return RsShare(range.tiles * per_tile, WARPS, warp); }  // units
+  // A warp's units: all parts' warps share the tiles' units.
+  __device__ __forceinline__ RsShare share(int warp) const {
+    return RsShare(range.tiles * per_tile, WARPS * op.parts, KIND == kRsSum ? blockIdx.x % op.parts * WARPS + warp : warp);
+  }
 
   __device__ __forceinline__ void set_tile(int i, int& tu, int& trow, int& tn0, int& tn1) const {
     int n;
@@ -655,7 +659,7 @@ struct RowStream {
           const int s_end = s.begin + s.count;
           if (s.count == 0 || s_end <= lo || s.begin >= hi) continue;
           whole = s.begin <= lo && s_end >= hi;  // (finished by its warp)
-          v += (s.begin > lo ? held_area(w) : slots + w * Z::SLOT)[sum_at(t, r)];
+          if (!whole) v += (s.begin > lo ? held_area(w) : slots + w * Z::SLOT)[sum_at(t, r)];
         }
         const int k = r % kRsRun;
         if (!whole && k < (r < kRsRun ? m0 : m1)) store(row0 + (r < kRsRun ? 0 : m0) + k, t, v);
