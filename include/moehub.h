@@ -352,12 +352,13 @@ int moe_layer(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* 
 /* The whole layer for a few tokens in ONE kernel launch (decoding): what moe_layer computes, for T <= MOE_FEW_MAX_TOKENS
  * (MOE_ERR_UNSUPPORTED beyond), bounded by reading the picked experts' weights once.  Arguments as for moe_layer; of the plan's
  * configuration T, H, E, K, F, dtype, renormalize and wait_limit_ns count (tp_shards changes nothing: an expert is computed
- * whole), identity experts are refused (MOE_ERR_ARG).  It differs from moe_layer in its rounding: logits are fp32 sums in an
- * order of their own (not the ascending chain of moe_route, so the pick between two experts whose logits agree to fp32 rounding
- * may differ), and an expert's output is not rounded to dtype before it is weighted and added.  The result does not depend on
- * the order in which the CTAs run, but a token's last bits may depend on which experts the other tokens of the batch pick (the
- * reading of the weights, and so the order of a sum, is shared out anew).  moe_layer_buffer 0, 1 and 3 (picks, their weights, rows per expert) hold the call's values
- * behind it, the other buffers anything.
+ * whole), identity experts are refused (MOE_ERR_ARG).  It differs from moe_layer in its rounding.  Logits are fp32 sums in an
+ * order of their own, not the ascending chain of moe_route: the pick between two experts whose logits agree to fp32 rounding
+ * may differ.  The SwiGLU results and the experts' outputs are not rounded to bf16 on the way; only y is.
+ * The result does not depend on the order in which the CTAs run, but a token's last bits may depend on which experts the other
+ * tokens of the batch pick (the reading of the weights, and so the order of a sum, is shared out anew).
+ * moe_layer_buffer 0, 1 and 3 (picks, their weights, rows per expert) hold the call's values behind it, the other buffers
+ * anything.
  * The launch is cooperative (all its CTAs are resident; one per SM): it starts when the SMs have room for all of it.  Its CTAs
  * wait for one another, each wait bounded by wait_limit_ns (0 = 2 s); on expiry the status word reads MOE_ERR_TIMEOUT and y holds
  * anything.  The plan's device has to be the current one (MOE_ERR_ARG). */

@@ -31,7 +31,7 @@ struct LayerFewParams {
   int T, H, E, K, F, renorm, tp;
   int slices, slice_cols;  // of the router's sums
   float* logits;           // [slices, T, E]
-  void* inter;             // [entries, 8, F]: the gate / up results of an entry's tokens
+  void* inter;             // the gate / up results of the entries' tokens, [entries, 8, F], on tensor cores followed by what rounding them left
   unsigned* sync;          // three barriers' counters, 128 bytes apart
   float* partial;          // [down_parts, T, H]: the outputs' parts, where there are several
   int down_parts;
@@ -65,14 +65,18 @@ __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which)
   __syncthreads();
 }
 
-constexpr int kLfSlots = 8;      // tokens of an entry
-constexpr int kLfEntries = 320;  // most entries: 256 experts, and 32 more eights of tokens among sixteen times 32 picks
+// Entries (see RsList): of the gate / up product one per used expert and eight tokens of it, of the down product one per expert and
+// `few` of them (four on tensor cores).  Most there can be: 256 experts, and one more per eight (four) of the remaining 256 of
+// sixteen times 32 picks.
+constexpr int kLfSlots = 8, kLfEntries = 288, kLfDownEntries = 320;
 struct LfShared {
   float w[kLfTokens * kLfPicks];                    // the picks' weights
   unsigned short used[kLfEntries];                  // an entry's expert, ascending
   unsigned char count[kLfEntries];
   unsigned char token[kLfEntries * kLfSlots];       // its tokens
   unsigned char pick[kLfEntries * kLfSlots];        // and which of a token's picks it is
+  unsigned short down_used[kLfDownEntries], down_row[kLfDownEntries];  // row: of the results, eight per gate / up entry
+  unsigned char down_count[kLfDownEntries];
 };
 constexpr int kLfBatch = 2;  // experts that a CTA scores at a time
 struct LfSelect {            // where the rows are streamed through later
@@ -80,7 +84,7 @@ struct LfSelect {            // where the rows are streamed through later
   int idx[kLfTokens * kLfPicks];
   unsigned mask[kMaxExperts];            // the tokens that picked an expert
   unsigned used[kMaxExperts / 32];       // bit per expert: picked at all,
-  unsigned many[kMaxExperts / 32];       // by more than kLfSlots tokens
+  unsigned many[3][kMaxExperts / 32];    // by more than 4, 8, 12 tokens
 };
 
 template <int N>
@@ -228,45 +232,59 @@ __device__ __forceinline__ void lf_pick(const LayerFewParams& p, LfShared& s, Lf
 // Before the barrier.
 __device__ __forceinline__ void lf_clear(LfSelect& q) {
   if (threadIdx.x < kMaxExperts) q.mask[threadIdx.x] = 0;
-  if (threadIdx.x < kMaxExperts / 32) q.used[threadIdx.x] = q.many[threadIdx.x] = 0;
+  if (threadIdx.x < kMaxExperts / 32) q.used[threadIdx.x] = q.many[0][threadIdx.x] = q.many[1][threadIdx.x] = q.many[2][threadIdx.x] = 0;
 }
 
-// Every CTA selects for itself; returns the number of entries: one per used expert and kLfSlots tokens of it.
-__device__ __forceinline__ int lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q) {
+// Every CTA selects for itself; n, n_down: the numbers of entries.  FEW: most tokens of one of the down product, 4 or 8.
+template <int FEW>
+__device__ __forceinline__ void lf_select(const LayerFewParams& p, LfShared& s, LfSelect& q, int& n, int& n_down) {
   const int tid = threadIdx.x;
   for (int t = tid / 32; t < p.T; t += blockDim.x / 32) {
     if (p.E <= 64) lf_pick<2>(p, s, q, t);
     else lf_pick<8>(p, s, q, t);
   }
   __syncthreads();
-  if (p.T > kLfSlots) {
-    if (tid < kMaxExperts && __popc(q.mask[tid]) > kLfSlots) atomicOr(&q.many[tid / 32], 1u << (tid % 32));
+  if (p.T > 4) {
+    if (tid < kMaxExperts)
+      for (int i = 0; i < 3; ++i)
+        if (__popc(q.mask[tid]) > 4 * (i + 1)) atomicOr(&q.many[i][tid / 32], 1u << (tid % 32));
     __syncthreads();
   }
-  int n = 0;
+  n = n_down = 0;
 #pragma unroll
-  for (int i = 0; i < kMaxExperts / 32; ++i) n += __popc(q.used[i]) + __popc(q.many[i]);
+  for (int i = 0; i < kMaxExperts / 32; ++i) {
+    const int used = __popc(q.used[i]), many = __popc(q.many[1][i]);
+    n += used + many;
+    n_down += used + many + (FEW == 4 ? __popc(q.many[0][i]) + __popc(q.many[2][i]) : 0);
+  }
   for (int a = tid; a < p.T * p.K; a += blockDim.x) {
     const int t = a / p.K, e = q.idx[a];
-    int at = 0;  // entries of the experts before e
+    int at = 0, down = 0;  // entries of the experts before e
 #pragma unroll
     for (int i = 0; i < kMaxExperts / 32; ++i) {
       const unsigned below = i < e / 32 ? 0xffffffffu : i == e / 32 ? (1u << (e % 32)) - 1u : 0u;
-      at += __popc(q.used[i] & below) + __popc(q.many[i] & below);
+      const int both = __popc(q.used[i] & below) + __popc(q.many[1][i] & below);
+      at += both;
+      down += both + (FEW == 4 ? __popc(q.many[0][i] & below) + __popc(q.many[2][i] & below) : 0);
     }
-    const int rank = __popc(q.mask[e] & ((1u << t) - 1u));
+    const int rank = __popc(q.mask[e] & ((1u << t) - 1u)), tokens = __popc(q.mask[e]);
     at += rank / kLfSlots;
+    down += rank / FEW;
     s.token[at * kLfSlots + rank % kLfSlots] = (unsigned char)t;
     s.pick[at * kLfSlots + rank % kLfSlots] = (unsigned char)(a - t * p.K);
     if (rank % kLfSlots == 0) {
       s.used[at] = (unsigned short)e;
-      s.count[at] = (unsigned char)min(kLfSlots, __popc(q.mask[e]) - rank);
+      s.count[at] = (unsigned char)min(kLfSlots, tokens - rank);
+    }
+    if (rank % FEW == 0) {
+      s.down_used[down] = (unsigned short)e;
+      s.down_row[down] = (unsigned short)(at * kLfSlots + rank % kLfSlots);
+      s.down_count[down] = (unsigned char)min(FEW, tokens - rank);
     }
   }
   if (blockIdx.x == 0)
     for (int e = tid; e < p.E * p.tp; e += blockDim.x) p.expert_count[e] = __popc(q.mask[e / p.tp]);
   __syncthreads();
-  return n;
 }
 
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
@@ -290,10 +308,13 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   else lf_router<X, kLfTokens>(p, q);
   lf_clear(q);
   grid_barrier(p, 0);
-  const RsList list{s.used, s.count, s.token, lf_select(p, s, q)};
+  int entries, down_entries;
+  lf_select<sizeof(X) == 2 ? 4 : kLfSlots>(p, s, q, entries, down_entries);
+  const RsList list{s.used, s.count, s.token, nullptr, entries}, down_list{s.down_used, s.down_count, nullptr, s.down_row, down_entries};
 
   // gate and up rows of the used experts
-  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, p.F, p.H, p.E, 1};
+  const long long rest = (long long)entries * kLfSlots * p.F;
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.E, 1};
   typedef RowStream<W, 1, kRsPairs> Up;
   Up up(gate_up, list, ring);
   auto finish_up = [&](int u, int row, int n0, int, const float*) {
@@ -302,16 +323,23 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
       if (Up::kMma && j % 4 >= 2) continue;
       const float upper = Up::kMma ? up.acc[Up::kMma ? j + 2 : j] : __shfl_down_sync(0xffffffffu, up.acc[j], kRsRun);
       const int t = up.token(j), f = up.row_of(j);
-      if (t < s.count[u] && f < n0 && (Up::kMma || (lane < kRsRun && up.is_first())))
-        ((X*)p.inter)[((size_t)u * kLfSlots + t) * p.F + row + f] = from_float<X>(lf_silu_mul(up.acc[j], upper));
+      if (t < s.count[u] && f < n0 && (Up::kMma || (lane < kRsRun && up.is_first()))) {
+        const float v = lf_silu_mul(up.acc[j], upper);
+        X* to = (X*)p.inter + ((size_t)u * kLfSlots + t) * p.F + row + f;
+        to[0] = from_float<X>(v);
+        if (Up::kMma) {
+          const float near = to_float(from_float<X>(v));
+          to[rest] = from_float<X>(fabsf(near) < INFINITY ? v - near : 0.0f);
+        }
+      }
     }
   };
-  up.run(nullptr, slots, [](int, int) { return 0.0f; }, finish_up);
+  up.run(nullptr, slots, [](int, int, int&) { return 0.0f; }, finish_up);
 
   // the outputs; the first down rows are on their way while the other CTAs finish
-  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, p.H, p.F, p.E, p.down_parts};
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, rest, p.H, p.F, p.E, p.down_parts};
   typedef RowStream<W, 1, kRsSum> Down;
-  Down down(down_op, list, ring);
+  Down down(down_op, down_list, ring);
   Down start = down;
   down.prefetch();
   __syncthreads();
@@ -327,7 +355,12 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
     if (r < (lane < kRsRun ? n0 : n1))
       for (int t = 0; t < p.T; ++t) store(row + (lane < kRsRun ? 0 : n0) + r, t, sums[Down::sum_at(t, lane)]);
   };
-  down.run(&start, slots, [&](int u, int slot) { return s.w[s.token[u * kLfSlots + slot] * p.K + s.pick[u * kLfSlots + slot]]; }, finish_down);
+  auto weight = [&](int u, int t, int& token) {
+    const int at = s.down_row[u] + t;
+    token = s.token[at];
+    return s.w[token * p.K + s.pick[at]];
+  };
+  down.run(&start, slots, weight, finish_down);
   __syncthreads();
   down.join_sums(slots, p.T, store);
   if (p.down_parts > 1) {
@@ -380,9 +413,9 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess) return MOE_ERR_CUDA;
   if (device != p->device) return MOE_ERR_ARG;
-  // the tokens' rows, and the gate / up results of at most two entries per expert, have 32-bit offsets
+  // numbers of units and of rows are 32-bit
   const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
-  if (c.T * c.H * eb >= 1ll << 32 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 32 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
+  if (c.T * c.H * eb >= 1ll << 31 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 31 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
   LayerFewParams q = {};
   q.x = x;
   q.wr = wr;

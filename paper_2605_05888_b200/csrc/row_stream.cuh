@@ -86,16 +86,21 @@ struct RsOperand {
   const __nv_bfloat16* s0;      // 4 bits: scales [matrices, C / group, N]
   const __nv_bfloat16* s1;
   const void* x;                // token rows [.., C]
+  long long x_rest;             // kRsSum on tensor cores: elements from a token's row to the row of what rounding it to bf16 left
   int N, C, matrices;           // matrices: all there are
   int parts;                    // kRsSum: CTAs that share a range of rows, each a part of the sums' terms (1: none)
 };
 
-// What is to be multiplied: entries, each a matrix and the up to 8 * NT tokens that it is for (a matrix with more tokens has
-// several entries, which share its reading in L2).  In shared memory.
+// What is to be multiplied: entries, each a matrix and the few tokens that it is for (a matrix with more tokens has several
+// entries, which share its reading in L2).  In shared memory.
+// An entry has up to 8 * NT tokens, a slot each; in kRsSum on tensor cores up to 4.  The tokens there are results of another product, and come as
+// two bf16 numbers each, what a value rounds to and what that left, in slots s and 4 + s: so the rounding does not show in the outputs (with
+// one number each they were 0.0024 from the sums in 64 bits, with two 0.0017, which is their own rounding), and costs nothing while slots are free.
 struct RsList {
   const unsigned short* used;   // matrix of an entry
   const unsigned char* count;   // its tokens
-  const unsigned char* token;   // [8 * NT] per entry: the rows of x (kRsSum: row entry * 8 * NT + slot, and this names the outputs)
+  const unsigned char* token;   // [8 * NT] per entry: the rows of x (not kRsSum)
+  const unsigned short* row;    // kRsSum: the first token's row of x, the others follow
   int n;
 };
 
@@ -220,7 +225,7 @@ struct RowStream {
     if constexpr (!k4Bit)
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i)
-        px[i] = (const char*)((const X*)op.x + (long long)x_row(u, i * 4 + lane / 8) * op.C) + (long long)chunk * kRsRowBytes + lane % 8 * 16;
+        px[i] = (const char*)((const X*)op.x + x_row(u, i * 4 + lane / 8)) + (long long)chunk * kRsRowBytes + lane % 8 * 16;
     if constexpr (k4Bit) {
       const int r = lane < 16 ? row : row1(row, n0);
       const long long first = (e * (op.C / F::GROUP) + (long long)chunk * F::GROUPS) * op.N + r;
@@ -228,10 +233,11 @@ struct RowStream {
       has_scale = lane % 16 < 9 && 2 * (lane % 16) < (lane < 16 ? n0 : n1) + (r & 1);
     }
   }
-  // The row of x of an entry's slot (one without a token: the first's).
-  __device__ __forceinline__ int x_row(int mu, int slot) const {
-    if (slot >= list.count[mu]) slot = 0;
-    return KIND == kRsSum ? mu * SLOTS + slot : (int)list.token[mu * SLOTS + slot];
+  static constexpr bool kTwo = KIND == kRsSum && kMma;  // tokens as two numbers
+  // Where the row of x for an entry's slot begins (for one without a token: the first's), in elements.
+  __device__ __forceinline__ long long x_row(int mu, int slot) const {
+    const int s = kTwo ? slot % 4 : slot, t = s < list.count[mu] ? s : 0;
+    return (long long)(KIND == kRsSum ? (int)list.row[mu] + t : (int)list.token[mu * SLOTS + t]) * op.C + (kTwo && slot >= 4 ? op.x_rest : 0);
   }
 
   __device__ __forceinline__ void advance() {
@@ -306,7 +312,7 @@ struct RowStream {
       const int bytes = chunk * kRsRowBytes + lane % 8 * 16 < (int)row_bytes() ? 16 : 0, limit = (int)list.count[u] - lane / 8;
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i)
-        if (i * 4 < limit) copy16(dst + Z::A + place(i * 4 + lane / 8, lane % 8), px[i], bytes);
+        if ((kTwo ? 0 : i * 4) < limit) copy16(dst + Z::A + place(i * 4 + lane / 8, lane % 8), px[i], bytes);
     }
   }
   // 4 bits: the lane's columns 8 * (lane % 4) and on of each 32, of half a chunk, of token lane / 4.
@@ -492,15 +498,15 @@ struct RowStream {
     m_tokens = list.count[m_u];
     if constexpr (k4Bit)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) m_x[t] = (const X*)op.x + (long long)x_row(m_u, 8 * t + lane / 4) * op.C + lane % 4 * 8;
+      for (int t = 0; t < NT; ++t) m_x[t] = (const X*)op.x + x_row(m_u, 8 * t + lane / 4) + lane % 4 * 8;
     if constexpr (k4Bit) m_base = list.used[m_u] * (op.C / F::GROUP);
   }
   // kRsSum: where a warp adds up its rows' results per token.  (The rows are swizzled so that the lanes of a fragment, which
   // hold eight rows of four tokens, hit different banks.)
   __device__ __forceinline__ static int sum_at(int t, int r) { return t * kRsTile + (r ^ ((t & 3) << 3)); }
 
-  // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, slot): of a token for an entry
-  // (kRsSum).  finish(u, row, n0, n1, sums): a whole tile, whose sums are in acc or (kRsSum) in shared memory at sum_at().
+  // start: a copy of this stream as it was before prefetch(), or nullptr without one.  weight(u, t, token&): of
+  // an entry's token t, and which it is among the outputs (kRsSum).  finish(u, row, n0, n1, sums): a whole tile, whose sums are in acc or (kRsSum) in shared memory at sum_at().
   // slots: shared memory, Z::SLOTS bytes.
   template <typename Weight, typename Finish>
   __device__ __forceinline__ void run(RowStream* start, float* slots, Weight weight, Finish finish) {
@@ -574,10 +580,13 @@ struct RowStream {
       if (KIND == kRsSum) {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
+          if (kTwo) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);  // slots s and 4 + s
           const int t = token(j);
           if (t < m_tokens && is_first()) {
-            float* to = slot + sum_at(list.token[m_u * SLOTS + t], run_of(j) * kRsRun + row_of(j));
-            *to = __fmaf_rn(weight(m_u, t), acc[j], *to);
+            int to_token;
+            const float w = weight(m_u, t, to_token);
+            float* to = slot + sum_at(to_token, run_of(j) * kRsRun + row_of(j));
+            *to = __fmaf_rn(w, acc[j], *to);
           }
           acc[j] = 0.0f;
         }

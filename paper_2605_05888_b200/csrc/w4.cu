@@ -278,8 +278,8 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
       if (lane == 0) entries = __popc(firsts);
     }
     __syncthreads();
-    const RsList list{used, count, token, entries};
-    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, p.N, p.C, p.experts, 1};
+    const RsList list{used, count, token, nullptr, entries};
+    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts, 1};
     typedef RowStream<W4<G>, NT, kRsRows> Stream;
     Stream rs(op, list, ring);
     auto finish = [&](int u, int row, int n0, int n1, const float*) {
@@ -291,7 +291,7 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
           p.y[(size_t)(m0 + token[u * SLOTS + t]) * p.N + row + (second ? n0 : 0) + r] = __float2bfloat16_rn(rs.acc[j]);
       }
     };
-    rs.run(nullptr, slots, [](int, int) { return 0.0f; }, finish);
+    rs.run(nullptr, slots, [](int, int, int&) { return 0.0f; }, finish);
     __syncthreads();
     rs.join(slots, finish);
     __syncthreads();

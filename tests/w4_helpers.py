@@ -75,7 +75,8 @@ def layer(x, wr, bias, wg, wu, wd, K, renorm, idx, dtype):
         s = g * sg * u
         # |silu'| <= 1.1; expf, the sum, the quotient and the product: a few roundings
         ds = 1.1 * dg * (u.abs() + du) + (g * sg).abs() * du + 8 * U32 * s.abs()
-        ds = ds + half * (s.abs() + ds)
+        # (held as fp32, or as two bf16 numbers: what a value rounds to, and what that left)
+        ds = ds + (half if dtype == torch.float32 else half * half) * (s.abs() + ds)
         down = wd(e)
         o, do = matvec(down, s)
         do = do + ds @ down.abs().T
