@@ -370,7 +370,8 @@ int moe_layer_few(moe_plan_t* plan, const void* d_x, const void* d_wr, const flo
  *   W[e,n,c] = scales[e, c/group, n] * (code(e,n,c) - 8),   code 0..15.
  * codes: [experts, N, C/2] bytes; the eight columns c..c+7 (c a multiple of 8) are one little-endian 32-bit word, whose
  * nibbles hold, from the least significant one on, columns c, c+2, c+4, c+6, c+1, c+3, c+5, c+7.
- * scales: [experts, C/group, N] bf16.  Both in DEVICE memory, 16-byte aligned. */
+ * scales: [experts, C/group, N] bf16.  Both in DEVICE memory, 16-byte aligned.
+ * C up to 2^25 (MOE_ERR_UNSUPPORTED beyond; so are other group sizes). */
 typedef struct {
   void* codes;
   void* scales;
@@ -387,7 +388,8 @@ int moe_layer_few_w4(moe_plan_t* plan, const void* d_x, const void* d_wr, const 
  * in: d_x [M,C] bf16, d_expert [M] int32 (NULL with experts == 1: that matrix for every row).  out: d_y [M,N] bf16.
  * A row whose id is outside [0, experts) is skipped: its y keeps its old contents.  Rows with the same matrix share its reading as
  * far as they are among the same MOE_FEW_MAX_TOKENS consecutive rows; M may be any number (with hundreds of rows
- * moe_w4_unpack and a matrix product are the better way).  Needs no plan and no workspace; runs on the current device. */
+ * moe_w4_unpack and a matrix product are the better way).  experts up to 65535, N up to 2^25 (MOE_ERR_UNSUPPORTED beyond).  Needs no plan
+ * and no workspace; runs on the current device. */
 int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const moe_w4_t* w, int32_t M, const void* d_x,
                   const int32_t* d_expert, void* d_y, void* stream);
 

@@ -91,6 +91,15 @@ def test_every_token_count(T, kind):
     Layer(T, 384, 12, 3, 320, dtype=FP32 if kind == "fp32" else BF16, group=64 if kind == "w4" else 0, seed=T).check()
 
 
+# more tokens on an expert than an entry holds, by one, by whole entries, all of them; outputs of a row or two per CTA with many terms
+# (several CTAs share them), one expert with as many columns as 40 of them
+@pytest.mark.parametrize("shape", [(16, 256, 2, 2, 128), (9, 512, 2, 1, 256), (13, 256, 3, 2, 384), (5, 128, 1, 1, 640), (16, 128, 20, 4, 4096),
+                                   (12, 384, 16, 6, 2048), (2, 256, 1, 1, 81920)], ids=str)
+@pytest.mark.parametrize("kind", ["bf16", "fp32", "w4"])
+def test_many_tokens_of_an_expert_and_few_outputs(shape, kind):
+    Layer(*shape, dtype=FP32 if kind == "fp32" else BF16, group=128 if kind == "w4" else 0, renorm=1, seed=3).check()
+
+
 def kinds(f):
     return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
 
@@ -245,6 +254,25 @@ def test_beside_a_kernel_that_fills_the_gpu(dtype, group):
     assert s.plan.moe_last_status() == (0, 0) and torch.equal(s.y, want)
 
 
+@kinds
+def test_output_in_the_place_of_the_tokens(dtype, group):
+    s = Layer(5, 512, 8, 2, 256, dtype=dtype, group=group)
+    want = s.call().clone()
+    assert torch.equal(s.call(y=s.x), want)
+
+
+def test_first_call_of_a_plan_inside_a_capture():
+    s = Layer(3, 512, 8, 2, 256, seed=4)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        s.call()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = s.y.clone()
+    assert torch.equal(s.check(), got)
+
+
 def test_wait_that_runs_out_is_reported():
     """A limit of one nanosecond: the barriers give up, the status says so, and the plan's counters are as before."""
     s = Layer(2, 512, 8, 2, 256, wait_limit_ns=1)
@@ -288,6 +316,7 @@ def test_calls_refuse_what_they_cannot_take():
         args = [s.x, s.wr, None, *s.w, s.y]
         args[missing] = args[missing].data_ptr() + 8
         assert code(s.plan.moe_layer_few, *args) == -2, missing
+    assert code(s.plan.moe_layer_few, s.x, s.wr, torch.zeros(4, device="cuda").data_ptr() + 2, *s.w, s.y) == -2
     other = Layer(4, 128, 4, 2, 64, group=32)
     with pytest.raises(ValueError):
         s.plan.moe_layer_few_w4(s.x, s.wr, None, q.w[0], other.w[1], q.w[2], s.y)

@@ -48,6 +48,7 @@ def test_calls_refuse_what_they_cannot_take(lib):
     assert matvec(w=None) == matvec(w=B.W4T(None, a)) == matvec(w=B.W4T(a, None)) == -1
     assert matvec(w=B.W4T(a + 8, a)) == matvec(w=B.W4T(a, a + 2)) == matvec(x=a + 8) == matvec(y=a + 4) == matvec(ids=a + 2) == -2
     assert matvec(M=-1) == matvec(x=None) == matvec(y=None) == -1
+    assert matvec(experts=65536, ids=a) == matvec(N=(1 << 25) + 1) == matvec(C=1 << 26) == pack(C=1 << 26) == unpack(C=1 << 26) == -3
     assert matvec(experts=2) == -1                                                       # several matrices, no ids
     assert matvec(M=0, x=None, y=None) == 0
     for call in (pack, unpack):
@@ -189,6 +190,12 @@ def test_matvec_one_matrix(group, N, groups, M):
 @pytest.mark.parametrize("N,groups", [(5, 1), (300, 3), (2817, 9)])
 def test_matvec_matrix_per_row(group, ids, N, groups):
     check_matvec(5, N, groups * group, group, len(ids), ids, seed=len(ids))
+
+
+@gpu
+@pytest.mark.parametrize("ids", [[1] * 19 + [0] * 3 + [1] * 10, [2] * 8 + [1] * 9, [0, 1] * 20, [3] * 40 + [-1] * 30 + [3] * 3])
+def test_matvec_more_rows_of_a_matrix_than_share_its_reading(ids):
+    check_matvec(5, 333, 512, 64, len(ids), ids)
 
 
 @gpu
