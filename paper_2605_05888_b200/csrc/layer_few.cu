@@ -1,8 +1,8 @@
 // The whole MoE layer (paper Section II-A, steps 1-5) for a few tokens in one launch, on bf16, fp32 or 4-bit expert weights
 // (moe_layer_few, moe_layer_few_w4 of include/moehub.h).
 //
-// As many CTAs as SMs, all resident (a cooperative launch), go through three parts with two grid-wide barriers between them (1.2 us
-// each):
+// As many CTAs as SMs, all resident (a cooperative launch), go through three parts with grid-wide barriers between them (1.2 us each;
+// a third one where CTAs share outputs):
 //   router   every CTA forms the logits of a few experts, or of slices of them where there are few experts
 //   gate/up  every CTA selects the picks for itself from the logits, and computes its share of the rows
 //            S[u, t, f] = silu(x_t Wg[e_u, f]) * (x_t Wu[e_u, f]) of the used experts e_0 < e_1 < ...
@@ -12,9 +12,11 @@
 //
 // Bound by reading the picked experts' weights once; for one token of small experts by latencies, which the trace of one Qwen-like token shows,
 // us: launch and router 2.4, barrier 1.2 of it, selection 1.7, gate/up 7 (46 MB), join and barrier 4, down 4 (23 MB), end 1.
-// Measured, device time, us, moe_layer (three launches or more) / this / the bytes at the copy rate: one Qwen-like token 31 / 22 / 10.6,
-// five Mixtral-like 430 / 343 / 315 (8 experts picked: 428), sixteen DeepSeek-like 1217 / 1256 expected bytes; 4 bits: one Qwen-like 20 / 2.8,
-// seven Mixtral-like 189 / 95, sixteen DeepSeek-like 620 / 350.
+// Measured, device time, us, moe_layer (three launches or more) / this / the picked experts' bytes at the copy rate.  bf16: Qwen-like 1 token
+// 27.6 / 22.6 / 10.5, 16 tokens 130 / 118 / 104; Mixtral-like 1 token 124 / 114 / 107, 5 tokens 379 / 340 / 340, 16 tokens 470 / 427 / 429;
+// DeepSeek-like 1 token 145 / 116 / 107, 16 tokens 1302 / 1223 / 1252; of 8 experts of 512 x 512, 4 tokens, 14.2 / 14.8 / 1.4 (latencies
+// alone).  fp32, 16 experts of 1020 x 2044, 3 tokens: 107 / 37 / 23.  4 bits (this / bytes): Qwen-like 1 token 20 / 2.8, Mixtral-like 7 tokens
+// 189 / 116, DeepSeek-like 16 tokens 620 / 350: bound by the instructions that unpack the codes (row_stream.cuh).
 #include "route_common.cuh"
 #include "row_stream.cuh"
 
@@ -73,7 +75,7 @@ __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which)
 }
 
 // Entries (see RsList): of the gate / up product one per used expert and eight tokens of it, of the down product one per expert and
-// `few` of them (four on tensor cores).  Most there can be: 256 experts, and one more per eight (four) of the remaining 256 of
+// `FEW` of them (four or eight on tensor cores).  Most there can be: 256 experts, and one more per eight (four) of the remaining 256 of
 // sixteen times 32 picks.
 constexpr int kLfSlots = 8, kLfEntries = 288, kLfDownEntries = 320;
 struct LfShared {
@@ -296,7 +298,11 @@ __device__ __forceinline__ void lf_select(const LayerFewParams& p, LfShared& s, 
 
 __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
-template <typename W>
+// DOWN: eights of token slots in the down product's entries, so that these have up to 4 * DOWN tokens as two numbers each.  2 where an expert
+// has at least two of more than four tokens on average (launch below): its entries of more than four tokens else read its down rows twice,
+// the second time from L2.  Measured, us, 1 / 2: Mixtral-like 16 tokens 476 / 427, 11 tokens 435 / 424, 8 tokens 402 / 404, 6 tokens 384 / 385,
+// Phi-like 16 tokens 330 / 324, 8 tokens 243.7 / 244.1, Qwen-like 6 tokens 66.7 / 68.1.
+template <typename W, int DOWN>
 __global__ void __launch_bounds__(RsSizes<W, 1>::THREADS, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   typedef typename RsFormat<W>::X X;
@@ -306,7 +312,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   static_assert(sizeof(LfSelect) <= Z::RING && Z::WARPS <= kLfMaxWarps && Z::THREADS >= kMaxExperts, "the selection's tables lie in the ring");
   LfSelect& q = *reinterpret_cast<LfSelect*>(dynamic);
   float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
-  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
+  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * Z::WARP_RING;
   const int lane = threadIdx.x % 32;
   if (blockIdx.x == 0 && threadIdx.x == 0) p.status[0] = p.status[1] = 0;
   if (p.T <= 1) lf_router<X, 1>(p, q);
@@ -316,7 +322,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   lf_clear(q);
   grid_barrier(p, 0);
   int entries, down_entries;
-  lf_select<sizeof(X) == 2 ? 4 : kLfSlots>(p, s, q, entries, down_entries);
+  lf_select<sizeof(X) == 2 ? 4 * DOWN : kLfSlots>(p, s, q, entries, down_entries);
   const RsList list{s.used, s.count, s.token, nullptr, entries}, down_list{s.down_used, s.down_count, nullptr, s.down_row, down_entries};
 
   // gate and up rows of the used experts
@@ -345,7 +351,8 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
 
   // the outputs; the first down rows are on their way while the other CTAs finish
   const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, rest, p.H, p.F, p.E, p.down_parts};
-  typedef RowStream<W, 1, kRsSum> Down;
+  typedef RowStream<W, DOWN, kRsSum> Down;
+  static_assert(RsSizes<W, DOWN>::WARP_RING == Z::WARP_RING && RsSizes<W, DOWN>::WARPS == Z::WARPS, "the ring is the same");
   Down down(down_op, down_list, ring);
   Down start = down;
   down.prefetch();
@@ -380,10 +387,10 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   }
 }
 
-template <typename W>
+template <typename W, int DOWN = 1>
 static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q, cudaStream_t st) {
   static SmemAttrOnce once;
-  auto kern = layer_few_kernel<W>;
+  auto kern = layer_few_kernel<W, DOWN>;
   cudaError_t e = ensure_dynamic_smem(kern, RsSizes<W, 1>::BYTES, p->device, once);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -454,7 +461,8 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
   cudaError_t e = group == 32 ? launch_cooperative<W4<32>>(p, q, st) : group == 64 ? launch_cooperative<W4<64>>(p, q, st) : group == 128 ? launch_cooperative<W4<128>>(p, q, st)
-                  : c.dtype == MOE_DTYPE_BF16 ? launch_cooperative<__nv_bfloat16>(p, q, st) : launch_cooperative<float>(p, q, st);
+                  : c.dtype != MOE_DTYPE_BF16 ? launch_cooperative<float>(p, q, st)
+                  : q.T > 4 && q.T * q.K >= 2 * q.E ? launch_cooperative<__nv_bfloat16, 2>(p, q, st) : launch_cooperative<__nv_bfloat16>(p, q, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     p->cuda_error = (int)e;

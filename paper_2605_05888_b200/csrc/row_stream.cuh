@@ -73,8 +73,9 @@ template <typename W, int NT> struct RsSizes {   // NT: token slots, in eights
   static constexpr int SLOT = 16 * kRsTile;      // floats of a warp's slot: its sums of a tile, or (kRsSum) 16 tokens' sums of its rows
   static constexpr int SLOTS = WARPS * SLOT * 4;
   static constexpr int ROOM = 218 * 1024 - SLOTS;  // (9 KB are left for the kernels' own tables)
-  static constexpr int STAGES = ROOM / (WARPS * STAGE) < 6 ? ROOM / (WARPS * STAGE) : 6;
-  static constexpr int RING = WARPS * STAGES * STAGE;
+  static constexpr int STAGES = ROOM / WARPS / STAGE < 6 ? ROOM / WARPS / STAGE : 6;
+  static constexpr int WARP_RING = ROOM / WARPS / 128 * 128;  // (of either NT's streams in one kernel)
+  static constexpr int RING = WARPS * WARP_RING;
   static constexpr int BYTES = RING + SLOTS;     // dynamic shared memory
   static_assert(STAGES >= 2 && REGS * 32 <= SLOT && STAGES * STAGE >= SLOT * 4, "a stage to fill beside one to read; a tile's sums fit a slot, a slot the ring");
 };
@@ -93,9 +94,10 @@ struct RsOperand {
 
 // What is to be multiplied: entries, each a matrix and the few tokens that it is for (a matrix with more tokens has several
 // entries, which share its reading in L2).  In shared memory.
-// An entry has up to 8 * NT tokens, a slot each; in kRsSum on tensor cores up to 4.  The tokens there are results of another product, and come as
-// two bf16 numbers each, what a value rounds to and what that left, in slots s and 4 + s: so the rounding does not show in the outputs (with
-// one number each they were 0.0024 from the sums in 64 bits, with two 0.0017, which is their own rounding), and costs nothing while slots are free.
+// An entry has up to 8 * NT tokens, a slot each; in kRsSum on tensor cores half as many.  The tokens there are results of another product, and
+// come as two bf16 numbers each, what a value rounds to and what that left, in slots s and 4 * NT + s: so the rounding does not show in
+// the outputs (with one number each they were 0.0024 from the sums in 64 bits, with two 0.0017, which is their own rounding), and
+// costs nothing while slots are free.
 struct RsList {
   const unsigned short* used;   // matrix of an entry
   const unsigned char* count;   // its tokens
@@ -236,8 +238,8 @@ struct RowStream {
   static constexpr bool kTwo = KIND == kRsSum && kMma;  // tokens as two numbers
   // Where the row of x for an entry's slot begins (for one without a token: the first's), in elements.
   __device__ __forceinline__ long long x_row(int mu, int slot) const {
-    const int s = kTwo ? slot % 4 : slot, t = s < list.count[mu] ? s : 0;
-    return (long long)(KIND == kRsSum ? (int)list.row[mu] + t : (int)list.token[mu * SLOTS + t]) * op.C + (kTwo && slot >= 4 ? op.x_rest : 0);
+    const int s = kTwo ? slot % (SLOTS / 2) : slot, t = s < list.count[mu] ? s : 0;
+    return (long long)(KIND == kRsSum ? (int)list.row[mu] + t : (int)list.token[mu * SLOTS + t]) * op.C + (kTwo && slot >= SLOTS / 2 ? op.x_rest : 0);
   }
 
   __device__ __forceinline__ void advance() {
@@ -312,7 +314,7 @@ struct RowStream {
       const int bytes = chunk * kRsRowBytes + lane % 8 * 16 < (int)row_bytes() ? 16 : 0, limit = (int)list.count[u] - lane / 8;
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i)
-        if ((kTwo ? 0 : i * 4) < limit) copy16(dst + Z::A + place(i * 4 + lane / 8, lane % 8), px[i], bytes);
+        if ((kTwo ? i * 4 % (SLOTS / 2) : i * 4) < limit) copy16(dst + Z::A + place(i * 4 + lane / 8, lane % 8), px[i], bytes);
     }
   }
   // 4 bits: the lane's columns 8 * (lane % 4) and on of each 32, of half a chunk, of token lane / 4.
@@ -580,16 +582,20 @@ struct RowStream {
       if (KIND == kRsSum) {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
-          if (kTwo) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);  // slots s and 4 + s
           const int t = token(j);
+          if (kTwo && NT == 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);  // slots s and 4 + s
+          if (kTwo && NT == 2 && j / 4 % NT == 0) acc[j] += acc[j + 4];            // s and 8 + s
           if (t < m_tokens && is_first()) {
             int to_token;
             const float w = weight(m_u, t, to_token);
             float* to = slot + sum_at(to_token, run_of(j) * kRsRun + row_of(j));
             *to = __fmaf_rn(w, acc[j], *to);
           }
-          acc[j] = 0.0f;
+          if (!(kTwo && NT == 2)) acc[j] = 0.0f;
         }
+        if (kTwo && NT == 2)
+#pragma unroll
+          for (int j = 0; j < REGS; ++j) acc[j] = 0.0f;
         __syncwarp();
         if (m_chunk == chunks && m_u + 1 < list.n) {
           ++m_u;
@@ -677,7 +683,7 @@ struct RowStream {
   }
   // kRsSum: warp w's sums of a tile that began before its share, in its ring.
   __device__ __forceinline__ float* held_area(int w) const {
-    return reinterpret_cast<float*>(__cvta_shared_to_generic(ring + (w - (int)threadIdx.x / 32) * (Z::STAGES * Z::STAGE)));
+    return reinterpret_cast<float*>(__cvta_shared_to_generic(ring + (w - (int)threadIdx.x / 32) * Z::WARP_RING));
   }
 
   // Of sum number j: the token's slot, the run, the row in it.

@@ -256,7 +256,7 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
   __shared__ unsigned char count[32], token[32 * SLOTS];
   __shared__ int entries;
   float* slots = reinterpret_cast<float*>(dynamic + Z::RING);
-  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * (Z::STAGES * Z::STAGE);
+  const uint32_t ring = smem_u32(dynamic) + threadIdx.x / 32 * Z::WARP_RING;
   const int lane = threadIdx.x % 32;
   for (int m0 = 0; m0 < p.M; m0 += batch) {
     const int rows = min(batch, p.M - m0);
