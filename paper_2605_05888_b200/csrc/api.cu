@@ -139,7 +139,7 @@ size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, s
   if (!c.identity_experts && c.T > 0 && c.T <= MOE_FEW_MAX_TOKENS) {
     t.few_logits = (float*)take(sizeof(float) * 256 * (size_t)c.T);
     t.few_sync = (unsigned*)take(sizeof(unsigned) * 96);
-    t.few_partial = (float*)take(sizeof(float) * kFewPartial * (size_t)c.T);
+    t.few_partial = (float*)take(sizeof(float) * (2 * (size_t)c.H + kFewPartial) * (size_t)c.T);
   }
   t.topk_idx = (int*)take(sizeof(int) * (size_t)c.T * c.K);
   t.topk_w = (float*)take(sizeof(float) * (size_t)c.T * c.K);

@@ -48,7 +48,8 @@ struct Scratch {          // device pointers carved out of the caller's workspac
   int route_slices;       // the slices of h that they are in (route_direct_kernel's: [route_slices, T, 256]); 0: another router
   float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens; else nullptr)
   unsigned* few_sync;     // [96]  its three grid barriers (every launch flips their highest bits)
-  float* few_partial;     // [kFewPartial, T] and its outputs in parts, where their rows are few (parts * H <= kFewPartial)
+  float* few_partial;     // [2 * H + kFewPartial, T] and its outputs in parts (a CTA of at most 256 has no less than half of another's units, so that
+                          // up to 2 * 256 / (H / 32) + 2 have some of 32 rows)
   float* route_wnorm2;    // [256]    squared norms of the router's weight rows, recomputed by every call (filter)
   // moe_layer's internal buffers
   int* topk_idx;

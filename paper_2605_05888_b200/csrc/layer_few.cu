@@ -42,8 +42,8 @@ struct LayerFewParams {
   float* logits;           // [slices, T, E]
   void* inter;             // the gate / up results of the entries' tokens, [entries, 8, F], on tensor cores followed by what rounding them left
   unsigned* sync;          // three barriers' counters, 128 bytes apart
-  float* partial;          // [down_parts, T, H]: the outputs' parts, where there are several
-  int down_parts;
+  float* partial;          // (split) [parts, T, H]: the outputs' parts, as many as CTAs have some of a tile
+  int split;               // of the outputs, see RsOperand
   int* topk_idx;           // the picks and rows per expert, as moe_layer leaves them (every TP shard listed)
   float* topk_w;
   int* expert_count;
@@ -327,7 +327,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
 
   // gate and up rows of the used experts
   const long long rest = (long long)entries * kLfSlots * p.F;
-  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.E, 1};
+  const RsOperand gate_up{p.wg.w, p.wu.w, p.wg.scales, p.wu.scales, p.x, 0, p.F, p.H, p.E, 0};
   typedef RowStream<W, 1, kRsPairs> Up;
   Up up(gate_up, list, ring);
   auto finish_up = [&](int u, int row, int n0, int, const float*) {
@@ -350,7 +350,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   up.run(nullptr, slots, [](int, int, int&) { return 0.0f; }, finish_up);
 
   // the outputs; the first down rows are on their way while the other CTAs finish
-  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, rest, p.H, p.F, p.E, p.down_parts};
+  const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, rest, p.H, p.F, p.E, p.split};
   typedef RowStream<W, DOWN, kRsSum> Down;
   static_assert(RsSizes<W, DOWN>::WARP_RING == Z::WARP_RING && RsSizes<W, DOWN>::WARPS == Z::WARPS, "the ring is the same");
   Down down(down_op, down_list, ring);
@@ -359,15 +359,15 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   __syncthreads();
   up.join(slots, finish_up);
   grid_barrier(p, 1);
-  float* part = p.down_parts > 1 ? p.partial + (size_t)(blockIdx.x % p.down_parts) * p.T * p.H : nullptr;
-  auto store = [&](int row, int t, float v) {
-    if (part != nullptr) part[(size_t)t * p.H + row] = v;
-    else ((X*)p.y)[(size_t)t * p.H + row] = from_float<X>(v);
+  auto store = [&](int row, int t, float v, int part) {
+    const size_t at = (size_t)t * p.H + row;
+    if (p.split) p.partial[(size_t)part * p.T * p.H + at] = v;
+    else ((X*)p.y)[at] = from_float<X>(v);
   };
   auto finish_down = [&](int, int row, int n0, int n1, const float* sums) {
     const int r = lane % kRsRun;
     if (r < (lane < kRsRun ? n0 : n1))
-      for (int t = 0; t < p.T; ++t) store(row + (lane < kRsRun ? 0 : n0) + r, t, sums[Down::sum_at(t, lane)]);
+      for (int t = 0; t < p.T; ++t) store(row + (lane < kRsRun ? 0 : n0) + r, t, sums[Down::sum_at(t, lane)], 0);
   };
   auto weight = [&](int u, int t, int& token) {
     const int at = s.down_row[u] + t;
@@ -377,13 +377,10 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   down.run(&start, slots, weight, finish_down);
   __syncthreads();
   down.join_sums(slots, p.T, store);
-  if (p.down_parts > 1) {
+  if (p.split) {
     grid_barrier(p, 2);
-    for (int i = blockIdx.x * Z::THREADS + threadIdx.x; i < p.T * p.H; i += gridDim.x * Z::THREADS) {
-      float v = 0.0f;
-      for (int j = 0; j < p.down_parts; ++j) v += __ldcg(p.partial + (size_t)j * p.T * p.H + i);
-      ((X*)p.y)[i] = from_float<X>(v);
-    }
+    for (int i = blockIdx.x * Z::THREADS + threadIdx.x; i < p.T * p.H; i += gridDim.x * Z::THREADS)
+      ((X*)p.y)[i] = from_float<X>(down.combine(p.partial + i, (size_t)p.T * p.H, (unsigned)i % (unsigned)p.H));
   }
 }
 
@@ -405,17 +402,16 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
 }
-// Where a CTA's share of the outputs is few rows, the loop over their columns is bound by its own latencies, not by bytes: several CTAs then share
-// more rows, each a part of the terms, and add up behind a third barrier, which costs about 2 us.  Measured, the down rows' part alone, us, one CTA / four
-// per range of rows: H 1024, F 2048, three tokens of 16 experts, bf16 7.7 / 3.2, fp32 14.6 / 7.4; F 4096, one token, fp32 9.9 / 4.5.
-static int down_parts(const moe_plan* p, int group) {
+// Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, about 4 us.
+static bool split_outputs(const moe_plan* p, int group) {
   const moe_config_t& c = p->cfg;
+  const int G = p->sm_count, picked = min(c.T * p->route_K, p->route_E), F = c.F * p->tp;
+  if ((c.H + kRsTile - 1ll) / kRsTile * kLfDownEntries * ((F + 31) / 32) >= 1ll << 31) return false;  // (numbers of units)
   const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
-  const double us = (double)min(c.T * p->route_K, p->route_E) * c.H * c.F * p->tp * bits / 8.0 / 6.0e6;  // of reading the down rows
-  int parts = 1;
-  while (parts < 16 && c.H * parts < 24 * p->sm_count) parts *= 2;
-  const double rows = (double)c.H / p->sm_count;
-  return us * (16.0 / rows - 1.0) > 4.0 ? parts : 1;
+  const double us = (double)picked * c.H * F * bits / 8.0 / 6.0e6;  // of reading the down rows
+  const double even = (double)c.H / G / kRsRun;                      // sixteen rows at a time that a CTA multiplies if shared
+  const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, alone = tiles * ((rows + tiles - 1) / tiles > kRsRun ? 2 : 1);
+  return (group > 0 ? 2.0 * us * (alone / even - 1.0) : us * (1.0 / even - 1.0)) > 4.0;
 }
 
 // The checks and the launch that both entry points share.
@@ -450,7 +446,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   const int unit = 8;
   q.slice_cols = ((c.H + q.slices - 1) / q.slices + unit - 1) / unit * unit;
   q.slices = (c.H + q.slice_cols - 1) / q.slice_cols;
-  q.down_parts = down_parts(p, group);
+  q.split = split_outputs(p, group);
   q.partial = p->s.few_partial;
   q.logits = p->s.few_logits;
   q.inter = p->s.inter;

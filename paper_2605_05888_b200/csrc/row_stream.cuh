@@ -89,7 +89,7 @@ struct RsOperand {
   const void* x;                // token rows [.., C]
   long long x_rest;             // kRsSum on tensor cores: elements from a token's row to the row of what rounding it to bf16 left
   int N, C, matrices;           // matrices: all there are
-  int parts;                    // kRsSum: CTAs that share a range of rows, each a part of the sums' terms (1: none)
+  int split;                    // kRsSum: 1: all CTAs' warps share all rows' units, so that a tile's sums may lie in several CTAs; 0: a CTA has rows of its own
 };
 
 // What is to be multiplied: entries, each a matrix and the few tokens that it is for (a matrix with more tokens has several
@@ -115,9 +115,14 @@ struct RsShare {
     begin = (int)(each * i + min(i, more));
     count = (int)(each + (i < more ? 1 : 0));
   }
+  // The share that thing `at` is in.
+  __device__ __forceinline__ static int of(unsigned n, unsigned parts, unsigned at) {
+    const unsigned each = n / parts, more = n - each * parts, line = more * (each + 1);
+    return (int)(at < line ? at / (each + 1) : more + (at - line) / each);
+  }
 };
 
-// The rows of one CTA (or of `parts` CTAs): its share of `used` entries' rows laid end to end (fewer than 2^31).  RT: rows of a tile.
+// The rows of one CTA (or of all, `groups` 1): its share of `used` entries' rows laid end to end (fewer than 2^31).  RT: rows of a tile.
 struct RsRange {
   int end, N, RT, first_u, first_row, first_len, first_tiles, full_tiles, tiles;
   __device__ __forceinline__ RsRange(int used, int N_, int RT_, unsigned group, unsigned groups) : N(N_), RT(RT_) {
@@ -188,7 +193,7 @@ struct RowStream {
   int lane;
 
   __device__ __forceinline__ RowStream(const RsOperand& op_, const RsList& list_, uint32_t ring_)
-      : op(op_), list(list_), range(KIND == kRsSum ? 1 : list_.n, op_.N, KIND == kRsPairs ? kRsRun : kRsTile, blockIdx.x / op_.parts, gridDim.x / op_.parts), ring(ring_) {
+      : op(op_), list(list_), range(KIND == kRsSum ? 1 : list_.n, op_.N, KIND == kRsPairs ? kRsRun : kRsTile, op_.split ? 0 : blockIdx.x, op_.split ? 1 : gridDim.x), ring(ring_) {
     lane = threadIdx.x % 32;
     chunks = (op.C + F::COLS - 1) / F::COLS;
     per_tile = KIND == kRsSum ? chunks * list.n : chunks;
@@ -204,10 +209,13 @@ struct RowStream {
     }
   }
 
-  // A warp's units: all parts' warps share the tiles' units.
   __device__ __forceinline__ RsShare share(int warp) const {
-    return RsShare(range.tiles * per_tile, WARPS * op.parts, KIND == kRsSum ? blockIdx.x % op.parts * WARPS + warp : warp);
+    const int first = KIND == kRsSum && op.split ? blockIdx.x * WARPS : 0;
+    return RsShare(range.tiles * per_tile, shares(), first + warp);
   }
+  __device__ __forceinline__ unsigned shares() const { return KIND == kRsSum && op.split ? WARPS * gridDim.x : WARPS; }
+  // (split) Which CTA has a unit.
+  __device__ __forceinline__ int cta_of(int unit) const { return RsShare::of(range.tiles * per_tile, shares(), unit) / WARPS; }
 
   __device__ __forceinline__ void set_tile(int i, int& tu, int& trow, int& tn0, int& tn1) const {
     int n;
@@ -657,11 +665,19 @@ struct RowStream {
     }
     finish(m_u, m_row, m_n0, m_n1, slots);
   }
-  // kRsSum: by all threads, a value each; store(row of y, token, value).
+  // kRsSum: by all threads, a value each; store(row of y, token, value, part).  (split) part: the CTA's number among those that have some of
+  // the tile (0 where finish gets a tile: it is whole); combine() adds them up.
   template <typename Store>
   __device__ __forceinline__ void join_sums(const float* slots, int tokens, Store store) {
-    for (int i = 0; i < range.tiles; ++i) {
-      const int lo = i * per_tile, hi = lo + per_tile;
+    int i = 0, end = range.tiles;
+    if (op.split) {
+      const RsShare first = share(0), last = share(WARPS - 1);
+      if (first.count == 0) return;
+      i = (unsigned)first.begin / (unsigned)per_tile;
+      end = (unsigned)(last.begin + last.count - 1) / (unsigned)per_tile + 1;
+    }
+    for (; i < end; ++i) {
+      const int lo = i * per_tile, hi = lo + per_tile, part = op.split ? blockIdx.x - cta_of(lo) : 0;
       int tu, row0, m0, m1;
       set_tile(i, tu, row0, m0, m1);
       for (int at = threadIdx.x; at < tokens * kRsTile; at += Z::THREADS) {
@@ -677,9 +693,17 @@ struct RowStream {
           if (!whole) v += (s.begin > lo ? held_area(w) : slots + w * Z::SLOT)[sum_at(t, r)];
         }
         const int k = r % kRsRun;
-        if (!whole && k < (r < kRsRun ? m0 : m1)) store(row0 + (r < kRsRun ? 0 : m0) + k, t, v);
+        if (!whole && k < (r < kRsRun ? m0 : m1)) store(row0 + (r < kRsRun ? 0 : m0) + k, t, v, part);
       }
     }
+  }
+  // (split) The sum of output `row`, whose CTAs' parts are at from[0], from[stride], ..
+  __device__ __forceinline__ float combine(const float* from, size_t stride, int row) const {
+    const int tile = RsShare::of(op.N, range.tiles, row), parts = cta_of((tile + 1) * per_tile - 1) - cta_of(tile * per_tile) + 1;
+    float v = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < parts; ++i) v += __ldcg(from + i * stride);
+    return v;
   }
   // kRsSum: warp w's sums of a tile that began before its share, in its ring.
   __device__ __forceinline__ float* held_area(int w) const {

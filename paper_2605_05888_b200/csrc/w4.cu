@@ -279,7 +279,7 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
     }
     __syncthreads();
     const RsList list{used, count, token, nullptr, entries};
-    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts, 1};
+    const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts, 0};
     typedef RowStream<W4<G>, NT, kRsRows> Stream;
     Stream rs(op, list, ring);
     auto finish = [&](int u, int row, int n0, int n1, const float*) {
