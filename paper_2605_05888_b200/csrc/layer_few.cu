@@ -52,17 +52,21 @@ struct LayerFewParams {
 };
 
 // Every CTA of the grid arrives exactly once per launch and barrier, also one whose wait ran out before: together they add 2^31, so
-// that the counter's highest bit flips with the last one and what is below it is as it was.  What was written before is visible
-// behind it (to loads that miss L1).
-__device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which) {
+// that the counter's highest bit flips with the last one and what is below it is as it was.  What was written before arrive() is
+// visible behind wait() (to loads that miss L1); arrive()'s result (of thread 0) is for wait().
+__device__ __forceinline__ unsigned grid_arrive(const LayerFewParams& p, int which) {
   __syncthreads();
+  unsigned before = 0;
   if (threadIdx.x == 0) {
-    unsigned* arrived = p.sync + 32 * which;
     const unsigned mine = blockIdx.x == 0 ? 0x80000000u - (gridDim.x - 1) : 1u;
-    unsigned before;
-    asm volatile("atom.add.release.gpu.global.u32 %0, [%1], %2;" : "=r"(before) : "l"(arrived), "r"(mine) : "memory");
+    asm volatile("atom.add.release.gpu.global.u32 %0, [%1], %2;" : "=r"(before) : "l"(p.sync + 32 * which), "r"(mine) : "memory");
+  }
+  return before;
+}
+__device__ __forceinline__ void grid_wait(const LayerFewParams& p, int which, unsigned before) {
+  if (threadIdx.x == 0) {
     unsigned long long t0 = 0;
-    while (!((before ^ (unsigned)ld_acquire(reinterpret_cast<int*>(arrived))) >> 31)) {
+    while (!((before ^ (unsigned)ld_acquire(reinterpret_cast<int*>(p.sync + 32 * which))) >> 31)) {
       const unsigned long long now = globaltimer();
       if (t0 == 0) t0 = now;
       if (now - t0 > p.wait_ns) {
@@ -73,6 +77,7 @@ __device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which)
   }
   __syncthreads();
 }
+__device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which) { grid_wait(p, which, grid_arrive(p, which)); }
 
 // Entries (see RsList): of the gate / up product one per used expert and eight tokens of it, of the down product one per expert and
 // `FEW` of them (four or eight on tensor cores).  Most there can be: 256 experts, and one more per eight (four) of the remaining 256 of
@@ -349,6 +354,10 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   };
   up.run(nullptr, slots, [](int, int, int&) { return 0.0f; }, finish_up);
 
+  __syncthreads();
+  up.join(slots, finish_up);
+  const unsigned arrived = grid_arrive(p, 1);
+
   // the outputs; the first down rows are on their way while the other CTAs finish
   const RsOperand down_op{p.wd.w, p.wd.w, p.wd.scales, p.wd.scales, p.inter, rest, p.H, p.F, p.E, p.split};
   typedef RowStream<W, DOWN, kRsSum> Down;
@@ -356,9 +365,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   Down down(down_op, down_list, ring);
   Down start = down;
   down.prefetch();
-  __syncthreads();
-  up.join(slots, finish_up);
-  grid_barrier(p, 1);
+  grid_wait(p, 1, arrived);
   auto store = [&](int row, int t, float v, int part) {
     const size_t at = (size_t)t * p.H + row;
     if (p.split) p.partial[(size_t)part * p.T * p.H + at] = v;
