@@ -409,16 +409,24 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
 }
-// Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, about 4 us.
+// Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, 3 to 4 us, and saves what a CTA with
+// rows of its own loses: with 4 bits, which are bound by instructions, to the rows that its sixteens lack (48.4 rows take as long as 64) and to
+// warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured, whole layers, us,
+// rows of its own / shared.  4 bits: DeepSeek-like 1 token 71.1 / 74.5, 2 tokens 114.6 / 114.8, 4 tokens 205 / 193, 16 tokens 622 / 560; Mixtral-like
+// 1 token 71.8 / 74.6, 7 tokens 190 / 186; Qwen-like 4 tokens 39.5 / 41.1, 16 tokens 78.8 / 73.7.  16 tokens, 64 experts of 1024 x 1024: 4 bits
+// 64 / 54, bf16 77 / 63, fp32 158 / 120; 1 token, 16 of 1024 x 2048: bf16 14.9 / 15.8, fp32 22.9 / 23.7, 3 tokens 25.8 / 26.7 and 40.6 / 38.6.
 static bool split_outputs(const moe_plan* p, int group) {
   const moe_config_t& c = p->cfg;
-  const int G = p->sm_count, picked = min(c.T * p->route_K, p->route_E), F = c.F * p->tp;
-  if ((c.H + kRsTile - 1ll) / kRsTile * kLfDownEntries * ((F + 31) / 32) >= 1ll << 31) return false;  // (numbers of units)
+  const int G = p->sm_count, picked = min(c.T * p->route_K, p->route_E), F = c.F * p->tp, all_tiles = (c.H + kRsTile - 1) / kRsTile;
+  if ((long long)all_tiles * kLfDownEntries * ((F + 31) / 32) >= 1ll << 31) return false;  // (numbers of units)
   const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
   const double us = (double)picked * c.H * F * bits / 8.0 / 6.0e6;  // of reading the down rows
-  const double even = (double)c.H / G / kRsRun;                      // sixteen rows at a time that a CTA multiplies if shared
-  const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, alone = tiles * ((rows + tiles - 1) / tiles > kRsRun ? 2 : 1);
-  return (group > 0 ? 2.0 * us * (alone / even - 1.0) : us * (1.0 / even - 1.0)) > 4.0;
+  if (group == 0) return us * ((double)G * kRsRun / c.H - 1.0) > 4.5;
+  // a warp's units of sixteen rows, alone and shared; the multiplication takes about twice as long as the reading
+  const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, runs = (rows + tiles - 1) / tiles > kRsRun ? 2 : 1;
+  const long long units = (long long)picked * ((F + RsFormat<W4<32>>::COLS - 1) / RsFormat<W4<32>>::COLS), warps = RsFormat<W4<32>>::WARPS;
+  const double alone = (double)((tiles * units + warps - 1) / warps * runs), shared = (double)((all_tiles * units + warps * G - 1) / (warps * G) * 2);
+  return 2.0 * us * (alone / shared - 1.0) > 4.5;
 }
 
 // The checks and the launch that both entry points share.

@@ -100,6 +100,16 @@ def test_many_tokens_of_an_expert_and_few_outputs(shape, kind):
     Layer(*shape, dtype=FP32 if kind == "fp32" else BF16, group=128 if kind == "w4" else 0, renorm=1, seed=3).check()
 
 
+# a row or ten per CTA, or eighteen and a half, of many terms: all CTAs share all outputs, and a number of rows that is no multiple of a tile's
+@pytest.mark.parametrize("T,H,E,K,F,kind", [(16, 1000, 16, 6, 4096, "bf16"), (5, 520, 24, 4, 4096, "bf16"), (9, 1500, 16, 4, 2052, "fp32"), (16, 36, 16, 4, 8192, "fp32"),
+                                            (16, 2720, 16, 4, 4096, "w4"), (7, 5024, 16, 4, 4096, "w4"), (3, 160, 16, 8, 8192, "w4")])
+def test_outputs_that_all_ctas_share(T, H, E, K, F, kind):
+    s = Layer(T, H, E, K, F, dtype=FP32 if kind == "fp32" else BF16, group=32 if kind == "w4" else 0, renorm=1, seed=T)
+    y = s.check().clone()
+    for _ in range(3):
+        assert torch.equal(s.call(), y)
+
+
 def kinds(f):
     return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
 
