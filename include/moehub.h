@@ -361,7 +361,8 @@ int moe_layer(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* 
  * anything.
  * The launch is cooperative (all its CTAs are resident; one per SM): it starts when the SMs have room for all of it.  Its CTAs
  * wait for one another, each wait bounded by wait_limit_ns (0 = 2 s); on expiry the status word reads MOE_ERR_TIMEOUT and y holds
- * anything.  The plan's device has to be the current one (MOE_ERR_ARG). */
+ * anything.  The plan's device has to be the current one (MOE_ERR_ARG).  x, and eight rows of F per picked expert and eight of its
+ * tokens, have to be smaller than 2 GB (MOE_ERR_UNSUPPORTED).  y may be x. */
 #define MOE_FEW_MAX_TOKENS 16
 int moe_layer_few(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* d_bias,
                   const void* d_wg, const void* d_wu, const void* d_wd, void* d_y, void* stream);
@@ -371,7 +372,7 @@ int moe_layer_few(moe_plan_t* plan, const void* d_x, const void* d_wr, const flo
  * codes: [experts, N, C/2] bytes; the eight columns c..c+7 (c a multiple of 8) are one little-endian 32-bit word, whose
  * nibbles hold, from the least significant one on, columns c, c+2, c+4, c+6, c+1, c+3, c+5, c+7.
  * scales: [experts, C/group, N] bf16.  Both in DEVICE memory, 16-byte aligned.
- * C up to 2^25 (MOE_ERR_UNSUPPORTED beyond; so are other group sizes). */
+ * C up to 2^25, N up to 2^30 (MOE_ERR_UNSUPPORTED beyond; so are other group sizes). */
 typedef struct {
   void* codes;
   void* scales;
@@ -386,10 +387,10 @@ int moe_layer_few_w4(moe_plan_t* plan, const void* d_x, const void* d_wr, const 
 
 /* Products of a few rows with 4-bit matrices: y[m,:] = W[d_expert[m]] x[m,:], m < M, fp32 sums, rounded once.
  * in: d_x [M,C] bf16, d_expert [M] int32 (NULL with experts == 1: that matrix for every row).  out: d_y [M,N] bf16.
- * A row whose id is outside [0, experts) is skipped: its y keeps its old contents.  Rows with the same matrix share its reading as
- * far as they are among the same MOE_FEW_MAX_TOKENS consecutive rows; M may be any number (with hundreds of rows
- * moe_w4_unpack and a matrix product are the better way).  experts up to 65535, N up to 2^25 (MOE_ERR_UNSUPPORTED beyond).  Needs no plan
- * and no workspace; runs on the current device. */
+ * A row whose id is outside [0, experts) is skipped: its y keeps its old contents.  One matrix is read once for every 8 rows (M <= 8)
+ * or 16; of several, rows with the same one share its reading by eights as far as they are among the same 32 consecutive rows.  M may be
+ * any number up to 2^30 (with hundreds of rows moe_w4_unpack and a matrix product are the better way), experts up to 65535, N up to 2^25
+ * (MOE_ERR_UNSUPPORTED beyond).  y is not x.  Needs no plan and no workspace; runs on the current device. */
 int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const moe_w4_t* w, int32_t M, const void* d_x,
                   const int32_t* d_expert, void* d_y, void* stream);
 

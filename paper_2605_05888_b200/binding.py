@@ -237,6 +237,9 @@ def moe_w4_matvec(w: W4, x, expert, y, stream=None) -> None:
         raise ValueError(f"x {x.dtype} {tuple(x.shape)} and y {y.dtype} {tuple(y.shape)} for matrices [{w.N}, {w.C}]")
     if expert is not None and (expert.dtype != torch.int32 or expert.shape != (M,)):
         raise ValueError("expert is int32 [M]")
+    on = w.codes.device
+    if x.device != on or y.device != on or (expert is not None and expert.device != on):
+        raise ValueError("x, y and expert are on the matrices' device")
     _call_on(w.codes, "moe_w4_matvec", stream, lib().moe_w4_matvec, w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y))
 
 
@@ -319,8 +322,9 @@ class Plan:
     def moe_layer_few_w4(self, x, wr, bias, wg: W4, wu: W4, wd: W4, y, stream=None):
         c = self.cfg
         if not (wg.experts == wu.experts == wd.experts == c.E and wg.group == wu.group == wd.group
-                and (wg.N, wg.C) == (wu.N, wu.C) == (wd.C, wd.N) == (c.F, c.H)):
-            raise ValueError("wg, wu: [E, F, H], wd: [E, H, F], one group size")
+                and (wg.N, wg.C) == (wu.N, wu.C) == (wd.C, wd.N) == (c.F, c.H)
+                and wg.codes.device == wu.codes.device == wd.codes.device == self.workspace.device):
+            raise ValueError("wg, wu: [E, F, H], wd: [E, H, F], one group size, on the plan's device")
         _check(lib().moe_layer_few_w4(self.handle, _ptr(x), _ptr(wr), _ptr(bias), wg.group, wg.ref, wu.ref, wd.ref, _ptr(y),
                                       _stream(stream)), "moe_layer_few_w4")
 

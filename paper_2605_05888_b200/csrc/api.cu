@@ -229,6 +229,18 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
     delete p;
     return MOE_ERR_CUDA;
   }
+  if (p->s.few_sync) {
+    // The one-launch layer's barriers count on from what the memset leaves: it is waited for, since the first call may come on a stream
+    // that the default stream does not order.  (Not prohibited by a capture on another stream.)
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    const cudaError_t e = cudaStreamSynchronize(0);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) {
+      delete p;
+      return MOE_ERR_CUDA;
+    }
+  }
   *out = p;
   return MOE_OK;
 }

@@ -53,7 +53,7 @@ struct LayerFewParams {
 
 // Every CTA of the grid arrives exactly once per launch and barrier, also one whose wait ran out before: together they add 2^31, so
 // that the counter's highest bit flips with the last one and what is below it is as it was.  What was written before arrive() is
-// visible behind wait() (to loads that miss L1); arrive()'s result (of thread 0) is for wait().
+// visible behind wait() (to loads that miss L1); arrive()'s result (of thread 0) is for wait().  late: the wait ran out (thread 0's).
 __device__ __forceinline__ unsigned grid_arrive(const LayerFewParams& p, int which) {
   __syncthreads();
   unsigned before = 0;
@@ -63,13 +63,14 @@ __device__ __forceinline__ unsigned grid_arrive(const LayerFewParams& p, int whi
   }
   return before;
 }
-__device__ __forceinline__ void grid_wait(const LayerFewParams& p, int which, unsigned before) {
+__device__ __forceinline__ void grid_wait(const LayerFewParams& p, int which, unsigned before, bool& late) {
   if (threadIdx.x == 0) {
     unsigned long long t0 = 0;
     while (!((before ^ (unsigned)ld_acquire(reinterpret_cast<int*>(p.sync + 32 * which))) >> 31)) {
       const unsigned long long now = globaltimer();
       if (t0 == 0) t0 = now;
       if (now - t0 > p.wait_ns) {
+        late = true;
         set_status(p.status, MOE_ERR_TIMEOUT, kWaitGrid);
         break;
       }
@@ -77,7 +78,7 @@ __device__ __forceinline__ void grid_wait(const LayerFewParams& p, int which, un
   }
   __syncthreads();
 }
-__device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which) { grid_wait(p, which, grid_arrive(p, which)); }
+__device__ __forceinline__ void grid_barrier(const LayerFewParams& p, int which, bool& late) { grid_wait(p, which, grid_arrive(p, which), late); }
 
 // Entries (see RsList): of the gate / up product one per used expert and eight tokens of it, of the down product one per expert and
 // `FEW` of them (four or eight on tensor cores).  Most there can be: 256 experts, and one more per eight (four) of the remaining 256 of
@@ -325,7 +326,8 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   else if (p.T <= 8) lf_router<X, 8>(p, q);
   else lf_router<X, kLfTokens>(p, q);
   lf_clear(q);
-  grid_barrier(p, 0);
+  bool late = false;
+  grid_barrier(p, 0, late);
   int entries, down_entries;
   lf_select<sizeof(X) == 2 ? 4 * DOWN : kLfSlots>(p, s, q, entries, down_entries);
   const RsList list{s.used, s.count, s.token, nullptr, entries}, down_list{s.down_used, s.down_count, nullptr, s.down_row, down_entries};
@@ -344,10 +346,13 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
       if (t < s.count[u] && f < n0 && (Up::kMma || (lane < kRsRun && up.is_first()))) {
         const float v = lf_silu_mul(up.acc[j], upper);
         X* to = (X*)p.inter + ((size_t)u * kLfSlots + t) * p.F + row + f;
-        to[0] = from_float<X>(v);
         if (Up::kMma) {
-          const float near = to_float(from_float<X>(v));
+          float near = to_float(from_float<X>(v));
+          if (fabsf(near) == INFINITY && fabsf(v) < INFINITY) near = __uint_as_float(__float_as_uint(v) & 0xffff0000u);  // (a number yet)
+          to[0] = from_float<X>(near);
           to[rest] = from_float<X>(fabsf(near) < INFINITY ? v - near : 0.0f);
+        } else {
+          to[0] = from_float<X>(v);
         }
       }
     }
@@ -365,7 +370,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   Down down(down_op, down_list, ring);
   Down start = down;
   down.prefetch();
-  grid_wait(p, 1, arrived);
+  grid_wait(p, 1, arrived, late);
   auto store = [&](int row, int t, float v, int part) {
     const size_t at = (size_t)t * p.H + row;
     if (p.split) p.partial[(size_t)part * p.T * p.H + at] = v;
@@ -385,10 +390,11 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
   __syncthreads();
   down.join_sums(slots, p.T, store);
   if (p.split) {
-    grid_barrier(p, 2);
+    grid_barrier(p, 2, late);
     for (int i = blockIdx.x * Z::THREADS + threadIdx.x; i < p.T * p.H; i += gridDim.x * Z::THREADS)
       ((X*)p.y)[i] = from_float<X>(down.combine(p.partial + i, (size_t)p.T * p.H, (unsigned)i % (unsigned)p.H));
   }
+  if (late) set_status(p.status, MOE_ERR_TIMEOUT, kWaitGrid);  // (once more: CTA 0 may have begun, and cleared it, after this one gave up)
 }
 
 template <typename W, int DOWN = 1>
@@ -440,7 +446,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   if (device != p->device) return MOE_ERR_ARG;
   // numbers of units and of rows are 32-bit
   const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
-  if (c.T * c.H * eb >= 1ll << 31 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 31 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
+  if ((long long)c.T * c.H * eb >= 1ll << 31 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 31 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
   LayerFewParams q = {};
   q.x = x;
   q.wr = wr;

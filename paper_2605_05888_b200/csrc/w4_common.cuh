@@ -17,7 +17,7 @@ __device__ __forceinline__ float w4_value(uint32_t word, int column) {
 // What the host checks of a matrix; returns MOE_OK or the error.
 inline int w4_check(const moe_w4_t* w, int64_t experts, int64_t N, int64_t C, int group) {
   if (w == nullptr || w->codes == nullptr || w->scales == nullptr || experts <= 0 || N <= 0 || C <= 0) return MOE_ERR_ARG;
-  if ((group != 32 && group != 64 && group != 128) || C > (1 << 25)) return MOE_ERR_UNSUPPORTED;
+  if ((group != 32 && group != 64 && group != 128) || C > (1 << 25) || N > (1 << 30)) return MOE_ERR_UNSUPPORTED;
   if (C % group != 0) return MOE_ERR_ARG;
   if ((reinterpret_cast<uintptr_t>(w->codes) | reinterpret_cast<uintptr_t>(w->scales)) & 15) return MOE_ERR_ALIGN;
   return MOE_OK;

@@ -283,6 +283,38 @@ def test_first_call_of_a_plan_inside_a_capture():
     assert torch.equal(s.check(), got)
 
 
+def test_plan_made_behind_other_work_and_first_called_on_a_stream_of_its_own():
+    """What plan creation leaves on the device is there before a stream that nothing orders can call."""
+    s = Layer(3, 512, 8, 2, 256, seed=4)
+    want, here = s.call().clone(), torch.cuda.Stream()
+    big = torch.randn(8192, 8192, device="cuda")
+    for fill in (0x7f, 0xff):
+        size = B.moe_workspace_bytes(s.plan.cfg) + 256
+        torch.full((size,), fill, dtype=torch.uint8, device="cuda")  # (freed: the plan's workspace is likely to be the same memory)
+        y = torch.zeros_like(s.y)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            big @ big
+        plan = B.Plan(s.plan.cfg)
+        s.call(y=y, plan=plan, stream=here)
+        here.synchronize()
+        assert plan.moe_last_status() == (0, 0) and torch.equal(y, want)
+
+
+def test_gate_results_that_only_fp32_holds():
+    """silu(g) u between bf16's largest number and fp32's is not an infinity on the way to a small output."""
+    s = Layer(1, 8, 1, 1, 8)
+    s.x.zero_()[0, :2] = 1.0
+    s.wr.zero_()
+    for w in s.w:
+        w.zero_()
+    s.w[0][0, 0, 0] = 2.0 ** 64
+    s.w[1][0, 0, :2] = torch.tensor([2.0 ** 64 * 255 / 256, 2.0 ** 64 * 3 / 1024], device="cuda")
+    s.w[2][0, 3, 0] = 2.0 ** -100
+    y = s.check()
+    assert y[0, 3].item() == 2.0 ** 28 and y.isfinite().all()
+
+
 def test_wait_that_runs_out_is_reported():
     """A limit of one nanosecond: the barriers give up, the status says so, and the plan's counters are as before."""
     s = Layer(2, 512, 8, 2, 256, wait_limit_ns=1)

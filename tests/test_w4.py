@@ -50,6 +50,7 @@ def test_calls_refuse_what_they_cannot_take(lib):
     assert matvec(M=-1) == matvec(x=None) == matvec(y=None) == -1
     assert matvec(experts=65536, ids=a) == matvec(N=(1 << 25) + 1) == matvec(C=1 << 26) == pack(C=1 << 26) == unpack(C=1 << 26) == -3
     assert matvec(experts=2) == -1                                                       # several matrices, no ids
+    assert matvec(M=(1 << 30) + 1) == matvec(N=(1 << 30) + 1) == pack(N=(1 << 30) + 1) == unpack(N=(1 << 30) + 1) == -3
     assert matvec(M=0, x=None, y=None) == 0
     for call in (pack, unpack):
         assert call(dtype=2) == call(dtype=-1) == call(w=None) == call(out=None) == -1
@@ -69,6 +70,9 @@ def test_matrices_that_do_not_belong_together_are_refused():
     x, y = torch.zeros(2, 128, dtype=bf), torch.zeros(2, 5, dtype=bf)
     ids = torch.zeros(2, dtype=torch.int32)
     for args in ((x.float(), ids, y), (x, ids, y.float()), (x[:, :64], ids, y), (x, ids, y[:, :4]), (x, ids[:1], y), (x, ids.long(), y)):
+        with pytest.raises(ValueError):
+            B.moe_w4_matvec(w, *args)
+    for args in ((x.to("meta"), ids, y), (x, ids.to("meta"), y), (x, ids, y.to("meta"))):
         with pytest.raises(ValueError):
             B.moe_w4_matvec(w, *args)
     with pytest.raises(ValueError):
