@@ -26,11 +26,6 @@ __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   f32x2 d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -82,23 +77,25 @@ __device__ __forceinline__ uint32_t w4_word_slow(const Eight<T>& v, float s) {
   for (int c = 0; c < 8; ++c) word |= w4_code(v[c], s) << w4_shift(c);
   return word;
 }
-// A word of codes, for a scale whose inverse is a number.  A product with the inverse and one correction (Markstein's) give the quotient rounded to fp32, also where the inverse is an ulp off; on the border
-// between two codes it is exact.  Where w is a bf16 number the quotient is nowhere else on a border: (2 k + 1) s / 2 has
-// 12 bits and w 8, so they are equal or 2^-12 of them apart.  Where w is an fp32 number it may be, and |w - k s|, which is exact (k s
-// has 12 bits and lies within s of w), is near s / 2 then: such words, one in a hundred thousand, are done with care.
+// A word of codes, for a scale whose inverse is a number.  The quotient is rounded twice: to multiples of 2^-14 (a product with the
+// inverse, off by less than 2^-19, and a sum in one step) and then to an integer, ties to even.  The first rounding puts a quotient that is on a border between
+// two codes, a multiple of 1/2, there exactly.  Where w is a bf16 number no other comes near one: (2 k + 1) s / 2 has 12
+// bits and w 8, so they are equal or 2^-12 of them apart, the quotients 2^-13.  Where w is an fp32 number it may, and |w - k s|, which is exact (k s
+// has 12 bits and lies within s of w), is near s / 2 then: such words, a few in a thousand, are done with care.
 template <typename T>
 __device__ __forceinline__ uint32_t w4_word(const Eight<T>& v, float s) {
   float inverse;
   asm("rcp.approx.f32 %0, %1;" : "=f"(inverse) : "f"(s));
   constexpr float kIntegers = 12582912.0f + 8.0f;  // 1.5 * 2^23: a sum with it is an integer, in the last bits; and the code's 8
-  const f32x2 inverse2 = pair(inverse, inverse), minus2 = pair(-s, -s), integers2 = pair(kIntegers, kIntegers), back2 = pair(-kIntegers, -kIntegers);
+  constexpr float kTies = 768.0f;                  // 1.5 * 2^9: a sum with it is a multiple of 2^-14
+  const f32x2 inverse2 = pair(inverse, inverse), minus2 = pair(-s, -s), ties2 = pair(kTies, kTies);
+  const f32x2 integers2 = pair(kIntegers - kTies, kIntegers - kTies), back2 = pair(-kIntegers, -kIntegers);
   uint32_t word = 0;
   float farthest = 0.0f;
 #pragma unroll
   for (int c = 0; c < 8; c += 2) {
     const f32x2 w = pair(v[c], v[c + 1]);
-    const f32x2 near = mul2(w, inverse2);
-    const f32x2 sum = add2(fma2(fma2(near, minus2, w), inverse2, near), integers2);
+    const f32x2 sum = add2(fma2(w, inverse2, ties2), integers2);
     float a, b;
     unpair(sum, a, b);
     word += __float_as_uint(a) * (1u << w4_shift(c)) + __float_as_uint(b) * (1u << w4_shift(c + 1));
@@ -140,7 +137,7 @@ w4_pack_kernel(const T* __restrict__ w, const PackShape p, uint32_t* __restrict_
       __nv_bfloat16 scale;
       uint32_t word;
       if (largest > 1e-28f && bits < 0x7f800000u) {
-        constexpr float seventh = 1.0f / 7.0f;  // (the quotient rounded to fp32, as in w4_word)
+        constexpr float seventh = 1.0f / 7.0f;  // (the quotient rounded to fp32: a product with the inverse and one correction, Markstein's)
         const float near = largest * seventh;
         scale = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-near, 7.0f, largest), seventh, near));
         word = w4_word(v[j], __bfloat162float(scale));
