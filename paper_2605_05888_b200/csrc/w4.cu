@@ -5,10 +5,15 @@
 namespace moehub {
 
 // ---- packing and unpacking ---------------------------------------------------------------------------------------------------
-// A warp takes a segment of a row (rows of few words: several), kPackUnroll words of eight columns per lane in flight, and is done: rows,
-// segments and matrices are the grid's three dimensions, so that no place has to be divided out and small matrices fill the GPU.
+// A warp takes a segment of a row (rows of few words: several), some words of eight columns per lane in flight: rows,
+// segments and matrices are the grid's three dimensions, so that no place has to be divided out and small matrices fill the GPU.  Packing goes
+// on to rows further down, whose words are loaded while these are coded; the grid is cut to a few rounds of CTAs for it.
+// Bound by HBM.  Measured on 8 matrices of 14336 x 4096, groups of 128, us: unpacking 187 (181 for the bytes at the copy rate), packing bf16
+// 227 (181): coding and the loads take turns in what is left (four words per lane in flight and no next ones 280; two, and one round of CTAs
+// 239, 8 rounds 227, 32 rounds 241; three CTAs per SM of 8 rounds 245, five 239; without the coding 243 of the 280).
 constexpr int kPackThreads = 256;
-constexpr int kPackUnroll = 4;
+constexpr int kPackUnroll = 2, kUnpackUnroll = 4;  // words per lane
+constexpr int kPackCtas = 4, kPackRounds = 8;      // of the packing kernel on an SM
 
 struct PackShape {
   int experts, N, C, lanes;  // lanes: of a row's segment, a power of two
@@ -111,42 +116,50 @@ __device__ __forceinline__ uint32_t w4_word(const Eight<T>& v, float s) {
 }
 
 template <typename T, int G>
-__global__ void __launch_bounds__(kPackThreads, 4)
+__global__ void __launch_bounds__(kPackThreads, kPackCtas)
 w4_pack_kernel(const T* __restrict__ w, const PackShape p, uint32_t* __restrict__ codes, __nv_bfloat16* __restrict__ scales) {
   constexpr int LANES = G / 8;  // of a group
-  const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
-  const int n = blockIdx.x * (kPackThreads / p.lanes) + threadIdx.x / p.lanes;
+  const int per_row = p.C / 8, lane = threadIdx.x % p.lanes, rows = kPackThreads / p.lanes;
   const int i0 = blockIdx.y * (p.lanes * kPackUnroll) + lane;
   for (int e = blockIdx.z; e < p.experts; e += gridDim.z) {
-    const size_t row = (size_t)e * p.N + n;
-    Eight<T> v[kPackUnroll];
+    auto load = [&](int n, Eight<T>(&v)[kPackUnroll]) {
 #pragma unroll
-    for (int j = 0; j < kPackUnroll; ++j) {
-      v[j].clear();
-      if (n < p.N && i0 + j * p.lanes < per_row) v[j].load(w + row * p.C + (size_t)(i0 + j * p.lanes) * 8);
-    }
-#pragma unroll
-    for (int j = 0; j < kPackUnroll; ++j) {
-      const int i = i0 + j * p.lanes;
-      uint32_t key = v[j].largest();
-#pragma unroll
-      for (int off = LANES / 2; off > 0; off >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, off));
-      if (n >= p.N || i >= per_row) continue;  // (whole groups: per_row is a multiple of LANES)
-      const uint32_t bits = Eight<T>::as_float(key);
-      const float largest = __uint_as_float(bits);
-      __nv_bfloat16 scale;
-      uint32_t word;
-      if (largest > 1e-28f && bits < 0x7f800000u) {
-        constexpr float seventh = 1.0f / 7.0f;  // (the quotient rounded to fp32: a product with the inverse and one correction, Markstein's)
-        const float near = largest * seventh;
-        scale = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-near, 7.0f, largest), seventh, near));
-        word = w4_word(v[j], __bfloat162float(scale));
-      } else {  // zeros, tiny numbers; a NaN or an infinity: NaN
-        scale = __float2bfloat16_rn(bits < 0x7f800000u ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
-        word = w4_word_slow(v[j], __bfloat162float(scale));
+      for (int j = 0; j < kPackUnroll; ++j) {
+        v[j].clear();
+        if (n < p.N && i0 + j * p.lanes < per_row) v[j].load(w + ((size_t)e * p.N + n) * p.C + (size_t)(i0 + j * p.lanes) * 8);
       }
-      __stcs(codes + row * per_row + i, word);
-      if (i % LANES == 0) scales[((size_t)e * (p.C / G) + i / LANES) * p.N + n] = scale;
+    };
+    Eight<T> v[kPackUnroll], next[kPackUnroll];
+    int n = blockIdx.x * rows + threadIdx.x / p.lanes;
+    load(n, v);
+    for (int left = p.N - blockIdx.x * rows; left > 0; left -= gridDim.x * rows, n += gridDim.x * rows) {
+      if (left > (int)gridDim.x * rows) load(n + gridDim.x * rows, next);
+      const size_t row = (size_t)e * p.N + n;
+#pragma unroll
+      for (int j = 0; j < kPackUnroll; ++j) {
+        const int i = i0 + j * p.lanes;
+        uint32_t key = v[j].largest();
+#pragma unroll
+        for (int off = LANES / 2; off > 0; off >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, off));
+        if (n >= p.N || i >= per_row) continue;  // (whole groups: per_row is a multiple of LANES)
+        const uint32_t bits = Eight<T>::as_float(key);
+        const float largest = __uint_as_float(bits);
+        __nv_bfloat16 scale;
+        uint32_t word;
+        if (largest > 1e-28f && bits < 0x7f800000u) {
+          constexpr float seventh = 1.0f / 7.0f;  // (the quotient rounded to fp32: a product with the inverse and one correction, Markstein's)
+          const float near = largest * seventh;
+          scale = __float2bfloat16_rn(__fmaf_rn(__fmaf_rn(-near, 7.0f, largest), seventh, near));
+          word = w4_word(v[j], __bfloat162float(scale));
+        } else {  // zeros, tiny numbers; a NaN or an infinity: NaN
+          scale = __float2bfloat16_rn(bits < 0x7f800000u ? __fdiv_rn(largest, 7.0f) : __int_as_float(0x7fc00000));
+          word = w4_word_slow(v[j], __bfloat162float(scale));
+        }
+        __stcs(codes + row * per_row + i, word);
+        if (i % LANES == 0) scales[((size_t)e * (p.C / G) + i / LANES) * p.N + n] = scale;
+      }
+#pragma unroll
+      for (int j = 0; j < kPackUnroll; ++j) v[j] = next[j];
     }
   }
 }
@@ -178,14 +191,14 @@ w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __rest
   constexpr int LANES = G / 8;
   const int per_row = p.C / 8, lane = threadIdx.x % p.lanes;
   const int n = blockIdx.x * (kPackThreads / p.lanes) + threadIdx.x / p.lanes;
-  const int i0 = blockIdx.y * (p.lanes * kPackUnroll) + lane;
+  const int i0 = blockIdx.y * (p.lanes * kUnpackUnroll) + lane;
   if (n >= p.N) return;
   for (int e = blockIdx.z; e < p.experts; e += gridDim.z) {
     const size_t row = (size_t)e * p.N + n;
-    uint32_t word[kPackUnroll];
-    __nv_bfloat16 s[kPackUnroll];
+    uint32_t word[kUnpackUnroll];
+    __nv_bfloat16 s[kUnpackUnroll];
 #pragma unroll
-    for (int j = 0; j < kPackUnroll; ++j) {
+    for (int j = 0; j < kUnpackUnroll; ++j) {
       const int i = i0 + j * p.lanes;
       if (i < per_row) {
         word[j] = __ldcs(codes + row * per_row + i);
@@ -193,24 +206,33 @@ w4_unpack_kernel(const uint32_t* __restrict__ codes, const __nv_bfloat16* __rest
       }
     }
 #pragma unroll
-    for (int j = 0; j < kPackUnroll; ++j) {
+    for (int j = 0; j < kUnpackUnroll; ++j) {
       const int i = i0 + j * p.lanes;
       if (i < per_row) w4_unpack8(word[j], s[j], w + row * p.C + (size_t)i * 8);
     }
   }
 }
 
+static int sm_count_now() {
+  int device = 0, sms = 0;
+  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
+  return sms;
+}
+
 // The grid, and the lanes of a row's segment (at least a group's).
-static dim3 pack_grid(PackShape& p, int group) {
+static dim3 pack_grid(PackShape& p, int group, int unroll) {
   p.lanes = group / 8;
   while (p.lanes < 32 && p.lanes < p.C / 8) p.lanes *= 2;
-  const int rows = kPackThreads / p.lanes, words = p.lanes * kPackUnroll;
+  const int rows = kPackThreads / p.lanes, words = p.lanes * unroll;
   return dim3((p.N + rows - 1) / rows, (p.C / 8 + words - 1) / words, p.experts < 65535 ? p.experts : 65535);
 }
 
 template <typename T>
 static cudaError_t launch_pack(const void* w, PackShape p, int group, const moe_w4_t& out, cudaStream_t st) {
-  const dim3 grid = pack_grid(p, group);
+  dim3 grid = pack_grid(p, group, kPackUnroll);
+  const int sms = sm_count_now();
+  if (sms <= 0) return cudaErrorUnknown;
+  grid.x = min(grid.x, max(1u, (unsigned)(sms * kPackCtas * kPackRounds) / (grid.y * grid.z)));
   auto kern = group == 32 ? w4_pack_kernel<T, 32> : group == 64 ? w4_pack_kernel<T, 64> : w4_pack_kernel<T, 128>;
   kern<<<grid, kPackThreads, 0, st>>>((const T*)w, p, (uint32_t*)out.codes, (__nv_bfloat16*)out.scales);
   return cudaGetLastError();
@@ -218,16 +240,10 @@ static cudaError_t launch_pack(const void* w, PackShape p, int group, const moe_
 
 template <typename T>
 static cudaError_t launch_unpack(const moe_w4_t& w, PackShape p, int group, void* out, cudaStream_t st) {
-  const dim3 grid = pack_grid(p, group);
+  const dim3 grid = pack_grid(p, group, kUnpackUnroll);
   auto kern = group == 32 ? w4_unpack_kernel<T, 32> : group == 64 ? w4_unpack_kernel<T, 64> : w4_unpack_kernel<T, 128>;
   kern<<<grid, kPackThreads, 0, st>>>((const uint32_t*)w.codes, (const __nv_bfloat16*)w.scales, p, (T*)out);
   return cudaGetLastError();
-}
-
-static int sm_count_now() {
-  int device = 0, sms = 0;
-  if (cudaGetDevice(&device) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) return 0;
-  return sms;
 }
 
 // ---- products with a few rows ------------------------------------------------------------------------------------------------

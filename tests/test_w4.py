@@ -129,6 +129,14 @@ def test_pack_and_unpack(dtype, group, shape):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("E,N,C,group", [(2, 3001, 4096, 128), (210, 745, 128, 32)])
+def test_pack_of_more_rows_than_the_grid(dtype, E, N, C, group):
+    g = torch.Generator(device="cuda").manual_seed(N)
+    check_pack(torch.empty(E, N, C, dtype=dtype, device="cuda").normal_(0.0, 0.02, generator=g), group)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_pack_on_the_borders_between_codes(dtype):
     """Weights at (k + 1/2) s and one step of their type on either side of it, for scales of every mantissa."""
     rows = []
