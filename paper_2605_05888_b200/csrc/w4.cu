@@ -8,9 +8,9 @@ namespace moehub {
 // A warp takes a segment of a row (rows of few words: several), some words of eight columns per lane in flight: rows,
 // segments and matrices are the grid's three dimensions, so that no place has to be divided out and small matrices fill the GPU.  Packing goes
 // on to rows further down, whose words are loaded while these are coded; the grid is cut to a few rounds of CTAs for it.
-// Bound by HBM.  Measured on 8 matrices of 14336 x 4096, groups of 128, us: unpacking 187 (181 for the bytes at the copy rate), packing bf16
-// 227 (181): coding and the loads take turns in what is left (four words per lane in flight and no next ones 280; two, and one round of CTAs
-// 239, 8 rounds 227, 32 rounds 241; three CTAs per SM of 8 rounds 245, five 239; without the coding 243 of the 280).
+// Measured on 8 matrices of 14336 x 4096, groups of 128, us: unpacking 187 (181 for the bytes at the copy rate: bound by HBM), packing bf16
+// 219 (181): bound by the instructions, about 100 per word (82 % of the issue slots; four words per lane in flight and no next ones 280; two,
+// and one round of CTAs 239, 8 rounds 227, 32 rounds 241; three CTAs per SM of 8 rounds 245, five 239; two buffers in turn instead of a copy 219).
 constexpr int kPackThreads = 256;
 constexpr int kPackUnroll = 2, kUnpackUnroll = 4;  // words per lane
 constexpr int kPackCtas = 4, kPackRounds = 8;      // of the packing kernel on an SM
@@ -129,11 +129,7 @@ w4_pack_kernel(const T* __restrict__ w, const PackShape p, uint32_t* __restrict_
         if (n < p.N && i0 + j * p.lanes < per_row) v[j].load(w + ((size_t)e * p.N + n) * p.C + (size_t)(i0 + j * p.lanes) * 8);
       }
     };
-    Eight<T> v[kPackUnroll], next[kPackUnroll];
-    int n = blockIdx.x * rows + threadIdx.x / p.lanes;
-    load(n, v);
-    for (int left = p.N - blockIdx.x * rows; left > 0; left -= gridDim.x * rows, n += gridDim.x * rows) {
-      if (left > (int)gridDim.x * rows) load(n + gridDim.x * rows, next);
+    auto code = [&](int n, const Eight<T>(&v)[kPackUnroll]) {
       const size_t row = (size_t)e * p.N + n;
 #pragma unroll
       for (int j = 0; j < kPackUnroll; ++j) {
@@ -158,8 +154,20 @@ w4_pack_kernel(const T* __restrict__ w, const PackShape p, uint32_t* __restrict_
         __stcs(codes + row * per_row + i, word);
         if (i % LANES == 0) scales[((size_t)e * (p.C / G) + i / LANES) * p.N + n] = scale;
       }
-#pragma unroll
-      for (int j = 0; j < kPackUnroll; ++j) v[j] = next[j];
+    };
+    Eight<T> v[kPackUnroll], next[kPackUnroll];  // (in turn)
+    const int step = gridDim.x * rows;
+    int n = blockIdx.x * rows + threadIdx.x / p.lanes, left = p.N - blockIdx.x * rows;
+    load(n, v);
+    while (true) {
+      if (left > step) load(n + step, next);
+      code(n, v);
+      if (left <= step) break;
+      if (left - step > step) load(n + 2 * step, v);
+      code(n + step, next);
+      if (left - step <= step) break;
+      left -= 2 * step;
+      n += 2 * step;
     }
   }
 }
