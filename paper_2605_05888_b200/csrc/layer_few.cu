@@ -343,7 +343,7 @@ layer_few_kernel(const __grid_constant__ LayerFewParams p) {
       if (Up::kMma && j % 4 >= 2) continue;
       const float upper = Up::kMma ? up.acc[Up::kMma ? j + 2 : j] : __shfl_down_sync(0xffffffffu, up.acc[j], kRsRun);
       const int t = up.token(j), f = up.row_of(j);
-      if (t < s.count[u] && f < n0 && (Up::kMma || (lane < kRsRun && up.is_first()))) {
+      if (t < s.count[u] && f < n0 && (Up::kMma || lane < kRsRun)) {
         const float v = lf_silu_mul(up.acc[j], upper);
         X* to = (X*)p.inter + ((size_t)u * kLfSlots + t) * p.F + row + f;
         if (Up::kMma) {
@@ -415,6 +415,17 @@ static cudaError_t launch_cooperative(const moe_plan* p, const LayerFewParams& q
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, q);
 }
+// Reading one product's rows of as many experts as the tokens can pick, at 6 TB/s.
+static double reading_us(const moe_plan* p, int group) {
+  const moe_config_t& c = p->cfg;
+  const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
+  return (double)min(c.T * p->route_K, p->route_E) * c.H * c.F * p->tp * bits / 8.0 / 6.0e6;
+}
+// (4 bits) Below this the small form of the code.  Measured, us, small / other: Qwen-like 1 token 19.1 / 20.5, 4 tokens 37.7 / 40.9, 16 tokens (15 us of
+// reading) 69.6 / 71.7, Mixtral-like 1 token (10 us) 66.9 / 68.0, 7 tokens (40 us) 186 / 178, DeepSeek-like 1 token (10 us) 69.0 / 67.2, 4 tokens (40 us)
+// 195 / 186, 16 tokens 570 / 543.
+constexpr double kSmallUs = 14.0;
+
 // Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, 3 to 4 us, and saves what a CTA with
 // rows of its own loses: with 4 bits, which are bound by instructions, to the rows that its sixteens lack (48.4 rows take as long as 64) and to
 // warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured, whole layers, us,
@@ -425,12 +436,11 @@ static bool split_outputs(const moe_plan* p, int group) {
   const moe_config_t& c = p->cfg;
   const int G = p->sm_count, picked = min(c.T * p->route_K, p->route_E), F = c.F * p->tp, all_tiles = (c.H + kRsTile - 1) / kRsTile;
   if ((long long)all_tiles * kLfDownEntries * ((F + 31) / 32) >= 1ll << 31) return false;  // (numbers of units)
-  const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
-  const double us = (double)picked * c.H * F * bits / 8.0 / 6.0e6;  // of reading the down rows
+  const double us = reading_us(p, group);
   if (group == 0) return us * ((double)G * kRsRun / c.H - 1.0) > 4.5;
   // a warp's units of sixteen rows, alone and shared; the multiplication takes about twice as long as the reading
-  const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, runs = (rows + tiles - 1) / tiles > kRsRun ? 2 : 1;
-  const long long units = (long long)picked * ((F + RsFormat<W4<32>>::COLS - 1) / RsFormat<W4<32>>::COLS), warps = RsFormat<W4<32>>::WARPS;
+  const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, runs = (rows + tiles - 1) / tiles > kRsRun || us >= kSmallUs ? 2 : 1;
+  const long long units = (long long)picked * ((F + RsFormat<W4<32, false>>::COLS - 1) / RsFormat<W4<32, false>>::COLS), warps = RsFormat<W4<32, false>>::WARPS;
   const double alone = (double)((tiles * units + warps - 1) / warps * runs), shared = (double)((all_tiles * units + warps * G - 1) / (warps * G) * 2);
   return 2.0 * us * (alone / shared - 1.0) > 4.5;
 }
@@ -477,7 +487,10 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.expert_count = p->s.expert_count;
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
-  cudaError_t e = group == 32 ? launch_cooperative<W4<32>>(p, q, st) : group == 64 ? launch_cooperative<W4<64>>(p, q, st) : group == 128 ? launch_cooperative<W4<128>>(p, q, st)
+  const bool small = reading_us(p, group) < kSmallUs;
+  cudaError_t e = group == 32    ? (small ? launch_cooperative<W4<32, true>>(p, q, st) : launch_cooperative<W4<32, false>>(p, q, st))
+                  : group == 64  ? (small ? launch_cooperative<W4<64, true>>(p, q, st) : launch_cooperative<W4<64, false>>(p, q, st))
+                  : group == 128 ? (small ? launch_cooperative<W4<128, true>>(p, q, st) : launch_cooperative<W4<128, false>>(p, q, st))
                   : c.dtype != MOE_DTYPE_BF16 ? launch_cooperative<float>(p, q, st)
                   : q.T > 4 && q.T * q.K >= 2 * q.E ? launch_cooperative<__nv_bfloat16, 2>(p, q, st) : launch_cooperative<__nv_bfloat16>(p, q, st);
   if (e != cudaSuccess) {

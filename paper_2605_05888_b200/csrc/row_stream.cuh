@@ -45,7 +45,10 @@ __device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint3
 }
 
 // ---- the weights' formats ----------------------------------------------------------------------------------------------------
-template <int GROUP> struct W4 {};  // (4 bits; float and __nv_bfloat16 name themselves)
+// 4 bits (float and __nv_bfloat16 name themselves).  SMALL: for little work, whose time the fetching of the code is a good part of (every SM
+// fetches it, also from HBM): half a chunk's code is not unrolled twice, and runs of at most eight rows have a form of their own.  For much
+// work that form costs more than it saves, since it is rarely taken.
+template <int GROUP, bool SMALL> struct W4 {};
 template <typename W> struct RsFormat;
 template <> struct RsFormat<__nv_bfloat16> {
   typedef __nv_bfloat16 X;                       // the tokens' type
@@ -57,8 +60,9 @@ template <> struct RsFormat<float> {
   typedef float X;
   static constexpr int COLS = 32, GROUP = 1, GROUPS = 0, WARPS = 8;
 };
-template <int G> struct RsFormat<W4<G>> {
+template <int G, bool S> struct RsFormat<W4<G, S>> {
   typedef __nv_bfloat16 X;
+  static constexpr bool SMALL = S;
   static constexpr int COLS = 256, GROUP = G, GROUPS = COLS / G;
   // Bound by the instructions that unpack the codes (12 of about 19 per word, with the MMA) and by their latencies: the more warps the better, as long as
   // their registers suffice.  Mixtral-like layer of 7 tokens, us, 8 / 12 / 16 / 18 warps: 266 / 206 / 181 / 204; of these 181, without unpacking
@@ -334,38 +338,31 @@ struct RowStream {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const uint4* from = reinterpret_cast<const uint4*>(m_x[t] + c);
-      if (c + HALF <= op.C) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) b[t][k] = KIND == kRsSum ? __ldcg(from + 4 * k) : __ldg(from + 4 * k);  // (kRsSum: written by this launch)
-      } else {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          b[t][k] = make_uint4(0, 0, 0, 0);
-          if (c + 32 * k < op.C) b[t][k] = KIND == kRsSum ? __ldcg(from + 4 * k) : __ldg(from + 4 * k);
-        }
+      for (int k = 0; k < 4; ++k) {
+        b[t][k] = make_uint4(0, 0, 0, 0);
+        if (c + 32 * k < op.C) b[t][k] = KIND == kRsSum ? __ldcg(from + 4 * k) : __ldg(from + 4 * k);  // (kRsSum: written by this launch)
       }
     }
   }
 
-  // A stage's products added to acc.  MT (tensor cores): 1 where the runs have at most 8 rows, else 2.  (Slots without a token hold anything: their
+  // A stage's products added to acc.  MT (tensor cores): 1 where the runs have at most 8 rows, else 2.  fp32: a lane per row, also where the
+  // runs have few rows.  (Slots without a token hold anything: their
   // sums are not read.)
   template <int MT>
   __device__ __forceinline__ void multiply(uint32_t a, int tokens) {
     if constexpr (!kMma) {
-      // MT 1, 2, 4: that many lanes share a row (of 16, 8, 4 per run), each with its part of the columns.  (With a lane per row a run of four rows
-      // keeps eight lanes of 32 busy: layer of 3 tokens, 16 experts of 1020 x 2044, 63 us; shared 45.)
-      constexpr int UNITS = 8 / MT;
-      float w[4 * UNITS];
+      float w[32];
 #pragma unroll
-      for (int c = 0; c < UNITS; ++c) Vec16<float>::unpack(lds128(a + place(lane / kRsRun * kRsRun + lane % kRsRun / MT, c * MT + lane % MT)), w + 4 * c);
+      for (int c = 0; c < 8; ++c) Vec16<float>::unpack(lds128(a + place(lane, c)), w + 4 * c);
 #pragma unroll
       for (int t = 0; t < SLOTS; ++t) {
         if (t >= tokens) break;
         float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-        for (int c = 0; c < UNITS; ++c) {
+        for (int c = 0; c < 8; ++c) {
           float v[4];
-          Vec16<float>::unpack(lds128(a + Z::A + place(t, c * MT + lane % MT)), v);
+          Vec16<float>::unpack(lds128(a + Z::A + place(t, c)), v);
           s0 = __fmaf_rn(w[4 * c], v[0], s0);
           s1 = __fmaf_rn(w[4 * c + 1], v[1], s1);
           s0 = __fmaf_rn(w[4 * c + 2], v[2], s0);
@@ -454,7 +451,7 @@ struct RowStream {
       flip = 2;
       if ((m_base + m_chunk * F::GROUPS) & 1) { o0 ^= 2u; o1 ^= 2u; }
     }
-#pragma unroll
+#pragma unroll (F::SMALL ? 1 : 2)
     for (int half = 0; half < 2; ++half) {
       if (m_chunk * F::COLS + half * HALF >= op.C) break;
       uint4 b[NT][4];
@@ -468,8 +465,8 @@ struct RowStream {
       }
       const uint32_t s0 = sc + half * (F::GROUPS * 36) + o0, s1 = sc + half * (F::GROUPS * 36) + 36 + o1;
       const uint32_t f0 = flip == 0 ? 0 : o0 ? (uint32_t)-2 : 2, f1 = flip == 0 ? 0 : o1 ? (uint32_t)-2 : 2;
-      if (m_n0 > 8) multiply4<2>(at ^ (half * 64), b, s0, s1, f0, f1);
-      else multiply4<1>(at ^ (half * 64), b, s0, s1, f0, f1);
+      if (F::SMALL && m_n0 <= 8) multiply4<1>(at ^ (half * 64), b, s0, s1, f0, f1);
+      else multiply4<2>(at ^ (half * 64), b, s0, s1, f0, f1);
     }
   }
   // Eight codes as exact bf16 integers code - 8, in pairs of neighbouring columns: 128 + code has the code in its last bits.
@@ -573,9 +570,7 @@ struct RowStream {
           if (m_n0 > 8) multiply<2>(stage, m_tokens);
           else multiply<1>(stage, m_tokens);
         } else {
-          if (m_n0 > 8) multiply<1>(stage, m_tokens);
-          else if (m_n0 > 4) multiply<2>(stage, m_tokens);
-          else multiply<4>(stage, m_tokens);
+          multiply<1>(stage, m_tokens);
         }
       }
       next = stage;
@@ -584,20 +579,13 @@ struct RowStream {
       const bool last = i + 1 == total;
       if (m_chunk < chunks && !last) continue;
       // the end of a matrix's columns, or of the share
-      if constexpr (!kMma) {
-#pragma unroll
-        for (int j = 0; j < REGS; ++j) {
-          if (row_lanes() >= 2) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 1);
-          if (row_lanes() >= 4) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);
-        }
-      }
       if (KIND == kRsSum) {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
           const int t = token(j);
           if (kTwo && NT == 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);  // slots s and 4 + s
           if (kTwo && NT == 2 && j / 4 % NT == 0) acc[j] += acc[j + 4];            // s and 8 + s
-          if (t < m_tokens && is_first()) {
+          if (t < m_tokens) {
             int to_token;
             const float w = weight(m_u, t, to_token);
             float* to = slot + sum_at(to_token, run_of(j) * kRsRun + row_of(j));
@@ -717,10 +705,7 @@ struct RowStream {
   // Of sum number j: the token's slot, the run, the row in it.
   __device__ __forceinline__ int token(int j) const { return kMma ? j / 4 % NT * 8 + lane % 4 * 2 + j % 2 : j; }
   __device__ __forceinline__ int run_of(int j) const { return kMma ? j / 2 % 2 : lane / kRsRun; }
-  __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun / row_lanes(); }
-  // fp32: how many lanes hold a row's sums, and the first of them.
-  __device__ __forceinline__ int row_lanes() const { return m_n0 > 8 ? 1 : m_n0 > 4 ? 2 : 4; }
-  __device__ __forceinline__ bool is_first() const { return kMma || lane % row_lanes() == 0; }
+  __device__ __forceinline__ int row_of(int j) const { return kMma ? j / (4 * NT) * 8 + lane / 4 : lane % kRsRun; }
 };
 
 }  // namespace moehub

@@ -267,10 +267,10 @@ struct W4MatvecParams {
 
 // Rows of x are taken `batch` at a time: 8 * NT of one matrix, or 32 of several; rows with the same matrix share its
 // reading by eights.
-template <int G, int NT>
-__global__ void __launch_bounds__(RsSizes<W4<G>, NT>::THREADS, 1)
+template <int G, int NT, bool SMALL>
+__global__ void __launch_bounds__(RsSizes<W4<G, SMALL>, NT>::THREADS, 1)
 w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
-  typedef RsSizes<W4<G>, NT> Z;
+  typedef RsSizes<W4<G, SMALL>, NT> Z;
   constexpr int SLOTS = 8 * NT;
   extern __shared__ __align__(128) unsigned char dynamic[];
   __shared__ unsigned short used[32];
@@ -301,7 +301,7 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
     __syncthreads();
     const RsList list{used, count, token, nullptr, entries};
     const RsOperand op{p.codes, p.codes, p.scales, p.scales, p.x + (size_t)m0 * p.C, 0, p.N, p.C, p.experts, 0};
-    typedef RowStream<W4<G>, NT, kRsRows> Stream;
+    typedef RowStream<W4<G, SMALL>, NT, kRsRows> Stream;
     Stream rs(op, list, ring);
     auto finish = [&](int u, int row, int n0, int n1, const float*) {
 #pragma unroll
@@ -319,17 +319,30 @@ w4_matvec_kernel(const __grid_constant__ W4MatvecParams p, int batch) {
   }
 }
 
-template <int G, int NT>
-static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
+template <int G, int NT, bool SMALL>
+static cudaError_t launch_matvec(const W4MatvecParams& q, int device, int sms, cudaStream_t st) {
+  typedef RsSizes<W4<G, SMALL>, NT> Z;
   static SmemAttrOnce once;
+  cudaError_t e = ensure_dynamic_smem(w4_matvec_kernel<G, NT, SMALL>, Z::BYTES, device, once);
+  if (e != cudaSuccess) return e;
+  w4_matvec_kernel<G, NT, SMALL><<<sms, Z::THREADS, Z::BYTES, st>>>(q, q.experts > 1 ? 32 : 8 * NT);
+  return cudaGetLastError();
+}
+
+// 16 rows of one matrix at a time (with eight warps, for the registers) where there are more than eight: groups of 128, 7168 x 7168, us, by
+// eights / by sixteens: 8 rows 12.6 / 16.6, 9 rows 22.4 / 16.9, 32 rows 44.0 / 31.7; of several matrices rows that share one are few (24 rows of 60
+// matrices of 2817 x 2048 27.0 / 33.9).  The small code where a CTA has no more than sixteen rows of the matrices: 1408 x 2048 5.0 / 5.5,
+// 16 rows 6.4 / 7.1; 7168 x 7168 12.6 / 12.1.
+template <int G>
+static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
-  if (e == cudaSuccess) e = ensure_dynamic_smem(w4_matvec_kernel<G, NT>, RsSizes<W4<G>, NT>::BYTES, device, once);
   if (e != cudaSuccess) return e;
   const int sms = sm_count_now();
   if (sms <= 0) return cudaErrorUnknown;
-  w4_matvec_kernel<G, NT><<<sms, RsSizes<W4<G>, NT>::THREADS, RsSizes<W4<G>, NT>::BYTES, st>>>(q, q.experts > 1 ? 32 : 8 * NT);
-  return cudaGetLastError();
+  const bool small = (long long)q.N * (q.experts > 1 ? min(q.M, 32) : 1) <= 16ll * sms;
+  if (q.M <= 8 || q.experts > 1) return small ? launch_matvec<G, 1, true>(q, device, sms, st) : launch_matvec<G, 1, false>(q, device, sms, st);
+  return small ? launch_matvec<G, 2, true>(q, device, sms, st) : launch_matvec<G, 2, false>(q, device, sms, st);
 }
 
 }  // namespace moehub
@@ -372,9 +385,7 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
     return MOE_ERR_ALIGN;
   const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, M};
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e;
-  if (M <= 8 || experts > 1) e = group == 32 ? launch_matvec<32, 1>(q, st) : group == 64 ? launch_matvec<64, 1>(q, st) : launch_matvec<128, 1>(q, st);
-  else e = group == 32 ? launch_matvec<32, 2>(q, st) : group == 64 ? launch_matvec<64, 2>(q, st) : launch_matvec<128, 2>(q, st);
+  const cudaError_t e = group == 32 ? launch_matvec<32>(q, st) : group == 64 ? launch_matvec<64>(q, st) : launch_matvec<128>(q, st);
   return e == cudaSuccess ? MOE_OK : MOE_ERR_CUDA;
 }
 
