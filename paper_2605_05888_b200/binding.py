@@ -63,7 +63,7 @@ class W4:
         if codes.device != scales.device:
             raise ValueError("codes and scales are on different devices")
         self.group = self.C // scales.shape[-2]
-        self.codes, self.scales = codes, scales
+        self.codes, self.scales, self.device, self.index = codes, scales, codes.device, codes.device.index
         self.struct = W4T(_ptr(codes), _ptr(scales))
         self.ref = ctypes.byref(self.struct)
 
@@ -210,13 +210,17 @@ def moe_combine_ep(cfg: MoeConfig, staging, rows_back, cap_rows: int, out_rows, 
                                 _ptr(status), _stream(stream)), "moe_combine_ep")
 
 
-def _call_on(t: torch.Tensor, where: str, stream, fn, *args) -> None:
-    """A call that takes no plan runs on the current device: it is made the tensors' one."""
-    if t.device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)), where)
+def _call_on(index: int, where: str, stream, fn, *args) -> None:
+    """A call that takes no plan runs on the current device: device `index` is made it."""
+    if index is None:
+        raise ValueError("the matrices are not on a CUDA device")
+    if index == torch.cuda.current_device():
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream))
     else:
-        with torch.cuda.device(t.device):
-            _check(fn(*args, _stream(stream)), where)
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream(stream))
+    if rc != MOE_OK:
+        raise MoeError(rc, where)
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -237,24 +241,23 @@ def moe_w4_matvec(w: W4, x, expert, y, stream=None) -> None:
         raise ValueError(f"x {x.dtype} {tuple(x.shape)} and y {y.dtype} {tuple(y.shape)} for matrices [{w.N}, {w.C}]")
     if expert is not None and (expert.dtype != torch.int32 or expert.shape != (M,)):
         raise ValueError("expert is int32 [M]")
-    on = w.codes.device
-    if x.device != on or y.device != on or (expert is not None and expert.device != on):
+    if x.device != w.device or y.device != w.device or (expert is not None and expert.device != w.device):
         raise ValueError("x, y and expert are on the matrices' device")
-    _call_on(w.codes, "moe_w4_matvec", stream, lib().moe_w4_matvec, w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y))
+    _call_on(w.index, "moe_w4_matvec", stream, lib().moe_w4_matvec, w.experts, w.N, w.C, w.group, w.ref, M, _ptr(x), _ptr(expert), _ptr(y))
 
 
 def moe_w4_pack(weights, out: W4, stream=None) -> None:
     """bf16 or fp32 weights [experts, N, C] into out's 4-bit codes and scales."""
     _w4_shape(out, weights)
     dtype = _dtype_code(weights)
-    _call_on(out.codes, "moe_w4_pack", stream, lib().moe_w4_pack, dtype, out.experts, out.N, out.C, out.group, _ptr(weights), out.ref)
+    _call_on(out.index, "moe_w4_pack", stream, lib().moe_w4_pack, dtype, out.experts, out.N, out.C, out.group, _ptr(weights), out.ref)
 
 
 def moe_w4_unpack(w: W4, out, stream=None) -> None:
     """The weights that w's codes stand for, into out [experts, N, C] (bf16 or fp32)."""
     _w4_shape(w, out)
     dtype = _dtype_code(out)
-    _call_on(w.codes, "moe_w4_unpack", stream, lib().moe_w4_unpack, dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out))
+    _call_on(w.index, "moe_w4_unpack", stream, lib().moe_w4_unpack, dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out))
 
 
 class Plan:

@@ -72,6 +72,10 @@ def test_matrices_that_do_not_belong_together_are_refused():
     for args in ((x.float(), ids, y), (x, ids, y.float()), (x[:, :64], ids, y), (x, ids, y[:, :4]), (x, ids[:1], y), (x, ids.long(), y)):
         with pytest.raises(ValueError):
             B.moe_w4_matvec(w, *args)
+    dense = torch.zeros(3, 5, 128, dtype=bf)
+    for call in (lambda: B.moe_w4_matvec(w, x, ids, y), lambda: B.moe_w4_pack(dense, w), lambda: B.moe_w4_unpack(w, dense)):  # all of it in host memory
+        with pytest.raises(ValueError):
+            call()
     for args in ((x.to("meta"), ids, y), (x, ids.to("meta"), y), (x, ids, y.to("meta"))):
         with pytest.raises(ValueError):
             B.moe_w4_matvec(w, *args)
@@ -129,7 +133,7 @@ def test_pack_and_unpack(dtype, group, shape):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("E,N,C,group", [(2, 3001, 4096, 128), (210, 745, 128, 32)])
+@pytest.mark.parametrize("E,N,C,group", [(2, 3001, 4096, 128), (210, 745, 128, 32), (70001, 2, 32, 32)])
 def test_pack_of_more_rows_than_the_grid(dtype, E, N, C, group):
     g = torch.Generator(device="cuda").manual_seed(N)
     check_pack(torch.empty(E, N, C, dtype=dtype, device="cuda").normal_(0.0, 0.02, generator=g), group)
