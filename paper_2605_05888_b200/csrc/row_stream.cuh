@@ -192,7 +192,7 @@ struct RowStream {
   int total, left;           // units of the share; how many are still to be copied
   // where the copies are
   int tile_i, chunk, u, row, n0, n1;  // chunk: of the matrix
-  const char *pa0, *pa1;     // the lane's first bytes of the unit
+  const char *pa0, *pa1;     // the lane's first bytes of the unit (4 bits: pa1 comes from pa0, for the registers)
   const char* ps;            // (4 bits, N even) the lane's scale word of the unit's first group
   bool has_scale;
   const char* px[2 * NT];    // (not 4 bits) the lane's bytes of tokens lane / 8, 4 + lane / 8, ..
@@ -238,7 +238,7 @@ struct RowStream {
     const long long e = list.used[u], ld = row_bytes();
     const long long at = (long long)(lane / 8) * ld + (long long)chunk * kRsRowBytes + lane % 8 * 16;
     pa0 = (const char*)op.w0 + (e * op.N + row) * ld + at;
-    pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
+    if constexpr (!k4Bit) pa1 = (const char*)op.w1 + (e * op.N + row1(row, n0)) * ld + at;
     if constexpr (!k4Bit)
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i)
@@ -260,7 +260,7 @@ struct RowStream {
   __device__ __forceinline__ void advance() {
     --left;
     pa0 += kRsRowBytes;
-    pa1 += kRsRowBytes;
+    if constexpr (!k4Bit) pa1 += kRsRowBytes;
     if constexpr (!k4Bit)
 #pragma unroll
       for (int i = 0; i < 2 * NT; ++i) px[i] += kRsRowBytes;
@@ -277,11 +277,16 @@ struct RowStream {
     }
   }
 
+  __device__ __forceinline__ const char* second() const {
+    if constexpr (!k4Bit) return pa1;
+    return KIND == kRsPairs ? pa0 + ((const char*)op.w1 - (const char*)op.w0) : pa0 + n0 * row_bytes();
+  }
+
   // The weights (and scales) of the current unit into a stage; zeros beyond the row.
   __device__ __forceinline__ void copy_weights(uint32_t dst) const {
     const long long step = RPI * row_bytes();
     const int bytes = chunk * kRsRowBytes + lane % 8 * 16 < (int)row_bytes() ? 16 : 0;
-    const char *a0 = pa0, *a1 = pa1;
+    const char *a0 = pa0, *a1 = second();
     const int limit0 = n0 - lane / 8, limit1 = n1 - lane / 8;
 #pragma unroll
     for (int i = 0; i < kRsRun / RPI; ++i) {
@@ -403,7 +408,7 @@ struct RowStream {
   __device__ __forceinline__ void multiply4(uint32_t at, const uint4 (&b)[NT][4], uint32_t s0, uint32_t s1, uint32_t f0, uint32_t f1) {
     constexpr int per_group = F::GROUP / 32;  // 32-column units
     float part[MT][NT][4];
-    uint32_t w[MT][4];
+    uint32_t w[MT][2][4];
     float e[MT][2][4 / per_group];  // the scales, ahead of their use
 #pragma unroll
     for (int q = 0; q < 4 / per_group; ++q)
@@ -413,16 +418,16 @@ struct RowStream {
         e[m][1][q] = scale(s1 + q * 72 + 16 * m + (q % 2 ? f1 : 0));
       }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (k % 2 == 0) {
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) ldsm4((k == 0 ? at : at ^ 32u) + 8 * m * kRsRowBytes, w[m]);  // (stages are 128-byte aligned)
-      }
+      for (int m = 0; m < MT; ++m) ldsm4((k == 0 ? at : at ^ 32u) + 8 * m * kRsRowBytes, w[m][k]);  // (stages are 128-byte aligned)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         uint32_t d0[4], d1[4];
-        dequantise(w[m][k % 2 * 2], d0);
-        dequantise(w[m][k % 2 * 2 + 1], d1);
+        dequantise(w[m][k / 2][k % 2 * 2], d0);
+        dequantise(w[m][k / 2][k % 2 * 2 + 1], d1);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           if (k % per_group == 0) mma16816_first(part[m][t], d0[0], d1[0], d0[1], d1[1], b[t][k].x, b[t][k].y);
