@@ -11,12 +11,12 @@
 // No row is copied, and no table is built that only a later launch would read.  The weights go through row_stream.cuh.
 //
 // Bound by reading the picked experts' weights once; for one token of small experts by latencies, which the trace of one Qwen-like token shows,
-// us: launch and router 2.4, barrier 1.2 of it, selection 1.7, gate/up 7 (46 MB), join and barrier 4, down 4 (23 MB), end 1.
+// us: launch and router 2.4, barrier 1.2 of it, selection 2, gate/up 7 (46 MB), joins 1, the others' arrival and the barrier 3, down 4 (23 MB), end 1.
 // Measured, device time, us, moe_layer (three launches or more) / this / the picked experts' bytes at the copy rate.  bf16: Qwen-like 1 token
-// 27.6 / 22.6 / 10.5, 16 tokens 130 / 118 / 104; Mixtral-like 1 token 124 / 114 / 107, 5 tokens 379 / 340 / 340, 16 tokens 470 / 427 / 429;
+// 27.6 / 21.7 / 10.5, 16 tokens 130 / 118 / 104; Mixtral-like 1 token 124 / 114 / 107, 5 tokens 379 / 340 / 340, 16 tokens 470 / 427 / 429;
 // DeepSeek-like 1 token 145 / 116 / 107, 16 tokens 1302 / 1223 / 1252; of 8 experts of 512 x 512, 4 tokens, 14.2 / 14.8 / 1.4 (latencies
-// alone).  fp32, 16 experts of 1020 x 2044, 3 tokens: 107 / 37 / 23.  4 bits (this / bytes): Qwen-like 1 token 20 / 2.8, Mixtral-like 7 tokens
-// 189 / 116, DeepSeek-like 16 tokens 620 / 350: bound by the instructions that unpack the codes (row_stream.cuh).
+// alone).  fp32, 16 experts of 1020 x 2044, 3 tokens: 107 / 38 / 23.  4 bits (this / bytes): Qwen-like 1 token 18.3 / 2.8, Mixtral-like 7 tokens
+// 170 / 116, DeepSeek-like 16 tokens 522 / 350: bound by the instructions that unpack the codes (row_stream.cuh).
 #include "route_common.cuh"
 #include "row_stream.cuh"
 
@@ -421,15 +421,15 @@ static double reading_us(const moe_plan* p, int group) {
   const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
   return (double)min(c.T * p->route_K, p->route_E) * c.H * c.F * p->tp * bits / 8.0 / 6.0e6;
 }
-// (4 bits) Below this the small form of the code.  Measured, us, small / other: Qwen-like 1 token 19.1 / 20.5, 4 tokens 37.7 / 40.9, 16 tokens (15 us of
-// reading) 69.6 / 71.7, Mixtral-like 1 token (10 us) 66.9 / 68.0, 7 tokens (40 us) 186 / 178, DeepSeek-like 1 token (10 us) 69.0 / 67.2, 4 tokens (40 us)
-// 195 / 186, 16 tokens 570 / 543.
-constexpr double kSmallUs = 14.0;
+// (4 bits) Below this the small form of the code.  Measured, us, small / other: Qwen-like 1 token 18.6 / 20.0, 4 tokens (4 us of reading) 35.4 / 39.3,
+// 16 tokens (15 us) 65.9 / 66.2, 16 tokens of 64 experts of 1024 x 1024 (6 us) 46.6 / 48.5, Mixtral-like 1 token (10 us) 62.1 / 62.0, 7 tokens (40 us)
+// 178.6 / 169.8, DeepSeek-like 1 token (10 us) 65.9 / 62.6, 4 tokens (40 us) 187 / 179, 16 tokens 552 / 523.
+constexpr double kSmallUs = 9.0;
 
 // Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, 3 to 4 us, and saves what a CTA with
 // rows of its own loses: with 4 bits, which are bound by instructions, to the rows that its sixteens lack (48.4 rows take as long as 64) and to
-// warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured, whole layers, us,
-// rows of its own / shared.  4 bits: DeepSeek-like 1 token 71.1 / 74.5, 2 tokens 114.6 / 114.8, 4 tokens 205 / 193, 16 tokens 622 / 560; Mixtral-like
+// warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured before the
+// loop over 4-bit rows took its present form, whole layers, us, rows of its own / shared.  4 bits: DeepSeek-like 1 token 71.1 / 74.5, 2 tokens 114.6 / 114.8, 4 tokens 205 / 193, 16 tokens 622 / 560; Mixtral-like
 // 1 token 71.8 / 74.6, 7 tokens 190 / 186; Qwen-like 4 tokens 39.5 / 41.1, 16 tokens 78.8 / 73.7.  16 tokens, 64 experts of 1024 x 1024: 4 bits
 // 64 / 54, bf16 77 / 63, fp32 158 / 120; 1 token, 16 of 1024 x 2048: bf16 14.9 / 15.8, fp32 22.9 / 23.7, 3 tokens 25.8 / 26.7 and 40.6 / 38.6.
 static bool split_outputs(const moe_plan* p, int group) {

@@ -65,7 +65,7 @@ template <int G, bool S> struct RsFormat<W4<G, S>> {
   static constexpr bool SMALL = S;
   static constexpr int COLS = 256, GROUP = G, GROUPS = COLS / G;
   // Bound by the instructions that unpack the codes (12 of about 19 per word, with the MMA) and by their latencies: the more warps the better, as long as
-  // their registers suffice.  Mixtral-like layer of 7 tokens, us, 8 / 12 / 16 / 18 warps: 266 / 206 / 181 / 204; of these 181, without unpacking
+  // their registers suffice.  Mixtral-like layer of 7 tokens, us, 8 / 12 / 16 / 18 warps, before the loop was made smaller: 266 / 206 / 181 / 204 (170 now); of the 181, without unpacking
   // 167, without the tokens' loads 166, without the scales 178, without all three 129 (116 for the bytes); 54 % of the issue slots, 51 % of the ALU.
   static constexpr int WARPS = 16;
 };
@@ -303,7 +303,7 @@ struct RowStream {
   __device__ __forceinline__ static int place(int r, int c) { return r * kRsRowBytes + ((c ^ (r & 7)) * 16); }
 
   // (4 bits) Whether N is odd: only in products by themselves.  (A layer's N are other matrices' C, multiples of the group; without the code for
-  // it a layer of 7 Mixtral-like tokens takes 175 us, with it 179.)
+  // it a layer of 7 Mixtral-like tokens takes 172 us, with it 179.)
   __device__ __forceinline__ bool odd() const { return KIND == kRsRows && (op.N & 1); }
 
   // Scale words: [group of the chunk][run][9], 16 rows from an even element on; half a warp per run.

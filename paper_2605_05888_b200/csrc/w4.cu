@@ -331,8 +331,8 @@ static cudaError_t launch_matvec(const W4MatvecParams& q, int device, int sms, c
 
 // 16 rows of one matrix at a time (with eight warps, for the registers) where there are more than eight: groups of 128, 7168 x 7168, us, by
 // eights / by sixteens: 8 rows 12.6 / 16.6, 9 rows 22.4 / 16.9, 32 rows 44.0 / 31.7; of several matrices rows that share one are few (24 rows of 60
-// matrices of 2817 x 2048 27.0 / 33.9).  The small code where a CTA has no more than sixteen rows of the matrices: 1408 x 2048 5.0 / 5.5,
-// 16 rows 6.4 / 7.1; 7168 x 7168 12.6 / 12.1.
+// matrices of 2817 x 2048 27.0 / 33.9).  The small code where a CTA has no more than sixteen rows of the matrices: 1408 x 2048, small / other,
+// 5.2 / 5.6, 16 rows 6.5 / 7.0; 7168 x 7168 16 rows 20.8 / 19.6; 24 rows of 60 matrices 27.6 / 27.0.
 template <int G>
 static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   int device = 0;
