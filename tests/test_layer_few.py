@@ -110,6 +110,12 @@ def test_outputs_that_all_ctas_share(T, H, E, K, F, kind):
         assert torch.equal(s.call(), y)
 
 
+# much 4-bit work (its own form of the code) with rows that end inside a chunk of 256 columns, entries of one token to eight
+@pytest.mark.parametrize("T,H,E,K,F,group", [(8, 2624, 16, 4, 4160, 64), (16, 2688, 16, 2, 4224, 128), (1, 4128, 16, 12, 4000, 32), (16, 128, 24, 6, 40064, 64)])
+def test_much_4bit_work_and_ragged_rows(T, H, E, K, F, group):
+    Layer(T, H, E, K, F, group=group, renorm=T % 2, bias=True, seed=T + group).check()
+
+
 def kinds(f):
     return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
 
