@@ -521,6 +521,9 @@ struct RowStream {
       for (int t = 0; t < NT; ++t) m_x[t] = (const X*)op.x + x_row(m_u, 8 * t + lane / 4) + lane % 4 * 8;
     if constexpr (k4Bit) m_base = list.used[m_u] * (op.C / F::GROUP);
   }
+  // Sums of tokens' first numbers and of what rounding left.  A weight that is an infinity makes the first an infinity, or a NaN where the
+  // token has a zero; the second, of numbers of any sign and zeros, would make a NaN of the infinity.
+  __device__ __forceinline__ static float with_rest(float near, float rest) { return fabsf(near) < INFINITY ? near + rest : near; }
   // kRsSum: where a warp adds up its rows' results per token.  (The rows are swizzled so that the lanes of a fragment, which
   // hold eight rows of four tokens, hit different banks.)
   __device__ __forceinline__ static int sum_at(int t, int r) { return t * kRsTile + (r ^ ((t & 3) << 3)); }
@@ -592,8 +595,8 @@ struct RowStream {
 #pragma unroll
         for (int j = 0; j < REGS; ++j) {
           const int t = token(j);
-          if (kTwo && NT == 1) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], 2);  // slots s and 4 + s
-          if (kTwo && NT == 2 && j / 4 % NT == 0) acc[j] += acc[j + 4];            // s and 8 + s
+          if (kTwo && NT == 1) acc[j] = with_rest(acc[j], __shfl_xor_sync(0xffffffffu, acc[j], 2));  // slots s and 4 + s
+          if (kTwo && NT == 2 && j / 4 % NT == 0) acc[j] = with_rest(acc[j], acc[j + 4]);            // s and 8 + s
           if (t < m_tokens) {
             int to_token;
             const float w = weight(m_u, t, to_token);

@@ -184,6 +184,40 @@ def test_nan_and_infinity_stay_with_their_token(dtype, group):
 
 
 @kinds
+@pytest.mark.parametrize("T,K", [(3, 2), (6, 8), (16, 2)])
+def test_infinite_down_weights_keep_their_sign(dtype, group, T, K):
+    """An infinity among the down weights makes an output the infinity that the products give, not a NaN: one per row here (4 bits: an
+    infinite scale, by which the group's sum is multiplied, of one code that is not 8), so that there is no other to take away from it."""
+    s = Layer(T, 256, 8, K, 320 if group < 64 else 384, dtype=dtype, group=group, seed=5)
+    want = s.call().clone()
+    idx, weight = s.plan.layer_tensor(0).tolist(), s.plan.layer_tensor(1)
+    assert (weight > 0).all()
+    e, rows = idx[0][0], [0, 7, 130, 255]
+    for i, (h, f) in enumerate(zip(rows, (3, 64, 131, 319))):
+        value = float("inf") if i % 2 else float("-inf")
+        if group:
+            s.w[2].scales[e, f // group, h] = value
+            q = torch.zeros(group, dtype=torch.int32, device="cuda")
+            q[f % group] = 3
+            lo = f // group * group // 2
+            s.w[2].codes[e, h, lo:lo + group // 2] = R.encode(q.unsqueeze(0))[0]
+        else:
+            s.w[2][e, h, f] = value
+    y = s.call()
+    gate, up = s.matrix(0)(e), s.matrix(1)(e)
+    for t in range(T):
+        if e not in idx[t]:
+            assert torch.equal(y[t], want[t])
+            continue
+        for i, (h, f) in enumerate(zip(rows, (3, 64, 131, 319))):
+            g, u = gate[f] @ s.x[t].double(), up[f] @ s.x[t].double()
+            sign = torch.sign(g * u) * (1 if i % 2 else -1)   # (silu has its argument's sign)
+            assert y[t, h] == sign * float("inf"), (t, h, y[t, h].item())
+        rest = [h for h in range(256) if h not in rows]
+        assert torch.equal(y[t, rest], want[t, rest])
+
+
+@kinds
 def test_same_bytes_every_time(dtype, group):
     s = Layer(10, 1024, 24, 3, 768, dtype=dtype, group=group)
     first = s.call().clone()
