@@ -450,10 +450,15 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
                      void* y, cudaStream_t st) {
   const moe_config_t& c = p->cfg;
   p->launches = 0;
-  if (c.T == 0) return MOE_OK;
   int device = -1;
   if (cudaGetDevice(&device) != cudaSuccess) return MOE_ERR_CUDA;
   if (device != p->device) return MOE_ERR_ARG;
+  if (c.T == 0) {  // no rows: no expert has any
+    return cudaMemsetAsync(p->s.status, 0, 2 * sizeof(int), st) == cudaSuccess &&
+                   cudaMemsetAsync(p->s.expert_count, 0, sizeof(int) * (size_t)c.E, st) == cudaSuccess
+               ? MOE_OK
+               : MOE_ERR_CUDA;
+  }
   // numbers of units and of rows are 32-bit
   const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
   if ((long long)c.T * c.H * eb >= 1ll << 31 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 31 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;

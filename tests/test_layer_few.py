@@ -373,6 +373,18 @@ def test_empty_batch():
     assert plan.moe_last_launch_count() == 0
 
 
+@pytest.mark.parametrize("tp", [1, 2])
+def test_empty_batch_leaves_no_counts_behind(tp):
+    """The rows per expert hold the call's values behind it, also where there are no rows."""
+    wr, w = torch.zeros(4, 64, dtype=BF16, device="cuda"), torch.zeros(4, 64, 64, dtype=BF16, device="cuda")
+    q = B.W4.empty(64, 64, 32, experts=4)
+    plan = B.Plan(B.make_config(0, 64, 4, 1, 2, 64, B.DTYPE_BF16, tp_shards=tp))
+    for call in (lambda: plan.moe_layer_few(None, wr, None, w, w, w, None), lambda: plan.moe_layer_few_w4(None, wr, None, q, q, q, None)):
+        plan.layer_tensor(3).fill_(55)
+        call()
+        assert plan.layer_tensor(3).tolist() == [0] * (4 * tp) and plan.moe_last_launch_count() == 0 and plan.moe_last_status() == (0, 0)
+
+
 def test_calls_refuse_what_they_cannot_take():
     s, q = Layer(4, 128, 4, 2, 64), Layer(4, 128, 4, 2, 64, group=64)
 
