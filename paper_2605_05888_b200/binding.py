@@ -7,6 +7,7 @@ missing or no CUDA device is present, calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -260,6 +261,18 @@ def moe_w4_unpack(w: W4, out, stream=None) -> None:
     _call_on(w.index, "moe_w4_unpack", stream, lib().moe_w4_unpack, dtype, w.experts, w.N, w.C, w.group, w.ref, _ptr(out))
 
 
+def _dense(what: str, t, shape: tuple, rows: int, dtype, device) -> int | None:
+    """_ptr(t) of a tensor that is of `shape` (or another one of rows * shape[-1] elements with the same last axis), dtype and device; others are
+    refused.  None and raw pointers are the library's to judge; of no rows nothing is read."""
+    if t is None or isinstance(t, int) or rows == 0:
+        return _ptr(t)
+    # (the common case first: these checks are host time of calls of some microseconds)
+    if t.dtype is dtype and (t.shape == shape or (t.shape[-1:] == shape[-1:] and t.numel() == rows * shape[-1])) and t.device == device:
+        assert t.is_contiguous()
+        return t.data_ptr()
+    raise ValueError(f"{what} is {dtype} {list(shape)} on {device}, not {t.dtype} {list(t.shape)} on {t.device}")
+
+
 class Plan:
     """Owns a moe_plan_t and the torch-allocated workspace it points into."""
 
@@ -283,6 +296,18 @@ class Plan:
             self.handle = None
 
     __del__ = close
+
+    @functools.cached_property
+    def _few(self):
+        """What the one-launch layers' kernel takes from the plan and not from the tensors: dtype, device, and the tensors' shapes and rows."""
+        c = self.cfg
+        return (torch.bfloat16 if c.dtype == DTYPE_BF16 else torch.float32, self.workspace.device, ((c.T, c.H), c.T), ((c.E, c.H), c.E), ((c.E,), 1),
+                None if c.identity_experts else ((c.E, c.F, c.H), c.E * c.F), ((c.E, c.H, c.F), c.E * c.H))
+
+    def _few_tokens(self, dtype, x, wr, bias, y):
+        _, device, tokens, router, biases, _, _ = self._few
+        return (_dense("x", x, *tokens, dtype, device), _dense("wr", wr, *router, dtype, device), _dense("bias", bias, *biases, torch.float32, device),
+                _dense("y", y, *tokens, dtype, device))
 
     # ---- the C ABI, same names -------------------------------------------------------------
     def moe_route(self, x, wr, bias, topk_idx, topk_w, stream=None):
@@ -319,17 +344,25 @@ class Plan:
                                _stream(stream)), "moe_layer")
 
     def moe_layer_few(self, x, wr, bias, wg, wu, wd, y, stream=None):
-        _check(lib().moe_layer_few(self.handle, _ptr(x), _ptr(wr), _ptr(bias), _ptr(wg), _ptr(wu), _ptr(wd), _ptr(y),
-                                   _stream(stream)), "moe_layer_few")
+        """The whole layer for cfg.T <= 16 tokens in one launch.  x, y [T, H], wr [E, H], wg, wu [E, F, H], wd [E, H, F] of the plan's dtype, bias
+        fp32 [E] or None, all on the plan's device; ValueError otherwise (raw device pointers are taken as they are)."""
+        dtype, device, _, _, _, up, down = self._few
+        px, pr, pb, py = self._few_tokens(dtype, x, wr, bias, y)
+        if up is None:  # (identity experts, which the library refuses)
+            pg, pu, pd = _ptr(wg), _ptr(wu), _ptr(wd)
+        else:
+            pg, pu, pd = _dense("wg", wg, *up, dtype, device), _dense("wu", wu, *up, dtype, device), _dense("wd", wd, *down, dtype, device)
+        _check(lib().moe_layer_few(self.handle, px, pr, pb, pg, pu, pd, py, _stream(stream)), "moe_layer_few")
 
     def moe_layer_few_w4(self, x, wr, bias, wg: W4, wu: W4, wd: W4, y, stream=None):
+        """moe_layer_few on 4-bit experts; x, wr and y are bf16."""
         c = self.cfg
+        px, pr, pb, py = self._few_tokens(torch.bfloat16, x, wr, bias, y)
         if not (wg.experts == wu.experts == wd.experts == c.E and wg.group == wu.group == wd.group
                 and (wg.N, wg.C) == (wu.N, wu.C) == (wd.C, wd.N) == (c.F, c.H)
                 and wg.codes.device == wu.codes.device == wd.codes.device == self.workspace.device):
             raise ValueError("wg, wu: [E, F, H], wd: [E, H, F], one group size, on the plan's device")
-        _check(lib().moe_layer_few_w4(self.handle, _ptr(x), _ptr(wr), _ptr(bias), wg.group, wg.ref, wu.ref, wd.ref, _ptr(y),
-                                      _stream(stream)), "moe_layer_few_w4")
+        _check(lib().moe_layer_few_w4(self.handle, px, pr, pb, wg.group, wg.ref, wu.ref, wd.ref, py, _stream(stream)), "moe_layer_few_w4")
 
     def moe_layer_host(self, h_x, wr, bias, wg, wu, wd, h_y, stream=None):
         """h_x, h_y: HOST tensors (pinned for asynchronous copies); weights: device tensors."""
