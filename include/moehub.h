@@ -174,7 +174,9 @@ int moe_workspace_bytes(const moe_config_t* cfg, size_t* out_bytes);
  * work.  (dtype fp32: as long as the same configuration needs with ffn_kernel 1 is enough; below
  * moe_workspace_bytes() the plan's experts are computed as with ffn_kernel 1.  Likewise for a router
  * that holds several sets of logits, from T*E*H = 3.2e8 on: with room for one set, and 1 KB, it
- * computes every chain, or filters all rows: see route_filter.)  Runs on the current CUDA device.
+ * computes every chain, or filters all rows: see route_filter.  Likewise for up to MOE_FEW_MAX_TOKENS
+ * tokens: with T*(8*H + 66560) + 512 bytes fewer the plan has every call but moe_layer_few and
+ * moe_layer_few_w4, which answer MOE_ERR_WORKSPACE.)  Waits for nothing.  Runs on the current CUDA device.
  * *out is freed by moe_plan_destroy. */
 int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, moe_plan_t** out);
 int moe_plan_destroy(moe_plan_t* plan);
@@ -359,6 +361,7 @@ int moe_layer(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* 
  * tokens of the batch pick (the reading of the weights, and so the order of a sum, is shared out anew).
  * moe_layer_buffer 0, 1 and 3 (picks, their weights, rows per expert) hold the call's values behind it, the other buffers
  * anything.
+ * A plan's first call is ordered behind what the default stream held when the plan was created (inside a capture the host waits for it).
  * The launch is cooperative (all its CTAs are resident; one per SM): it starts when the SMs have room for all of it.  Its CTAs
  * wait for one another, each wait bounded by wait_limit_ns (0 = 2 s); on expiry the status word reads MOE_ERR_TIMEOUT and y holds
  * anything.  The plan's device has to be the current one (MOE_ERR_ARG).  x, and eight rows of F per picked expert and eight of its

@@ -89,8 +89,9 @@ int check_config(const moe_config_t* user, Geometry* g) {
 
 // Lays the scratch out in the workspace; with base == nullptr only measures it.  roomy: with what the fp32 experts on tensor cores
 // and the router that fetches its candidates' rows take for themselves, where they are used (a plan without has the kernels that
-// want no more than before them: FMAs, and the chains or the filter over all rows).
-size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, size_t* counters_bytes, bool roomy = true) {
+// want no more than before them: FMAs, and the chains or the filter over all rows).  few: with what the one-launch layer takes (a plan
+// without has every other call).
+size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, size_t* counters_bytes, bool roomy = true, bool few = true) {
   size_t off = 0;
   auto take = [&](size_t bytes) -> char* {
     char* ptr = base ? base + off : nullptr;
@@ -136,11 +137,6 @@ size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, s
   const size_t slabs = direct ? (size_t)t.route_slices : 1;
   t.route_logits = filter || (chains && experts > 64) ? (float*)take(sizeof(float) * slabs * (size_t)(c.T > 0 ? c.T : 1) * 256) : nullptr;
   t.route_wnorm2 = filter ? (float*)take(sizeof(float) * 256) : nullptr;
-  if (!c.identity_experts && c.T > 0 && c.T <= MOE_FEW_MAX_TOKENS) {
-    t.few_logits = (float*)take(sizeof(float) * 256 * (size_t)c.T);
-    t.few_sync = (unsigned*)take(sizeof(unsigned) * 96);
-    t.few_partial = (float*)take(sizeof(float) * (2 * (size_t)c.H + kFewPartial) * (size_t)c.T);
-  }
   t.topk_idx = (int*)take(sizeof(int) * (size_t)c.T * c.K);
   t.topk_w = (float*)take(sizeof(float) * (size_t)c.T * c.K);
   t.recv = take(pool_rows * c.H * g.eb);
@@ -152,6 +148,11 @@ size_t carve(const moe_config_t& c, const Geometry& g, char* base, Scratch* s, s
   for (int b = 0; b < 2; ++b) {
     t.x_stage[b] = take((size_t)c.T * c.H * g.eb);
     t.y_stage[b] = take((size_t)c.T * c.H * g.eb);
+  }
+  if (few && !c.identity_experts && c.T > 0 && c.T <= MOE_FEW_MAX_TOKENS) {
+    t.few_logits = (float*)take(sizeof(float) * 256 * (size_t)c.T);
+    t.few_sync = (unsigned*)take(sizeof(unsigned) * kFewSync);
+    t.few_partial = (float*)take(sizeof(float) * (2 * (size_t)c.H + kFewPartial) * (size_t)c.T);
   }
   if (s) *s = t;
   return off;
@@ -189,8 +190,14 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
   if (rc != MOE_OK) return rc;
   if (!d_workspace) return MOE_ERR_ARG;
   if (reinterpret_cast<uintptr_t>(d_workspace) % kAlign != 0) return MOE_ERR_WORKSPACE;
-  const bool roomy = bytes >= carve(g.eff, g, nullptr, nullptr, nullptr);
-  if (!roomy && bytes < carve(g.eff, g, nullptr, nullptr, nullptr, false)) return MOE_ERR_WORKSPACE;
+  // the most that the workspace has room for; the one-launch layer, of which only its own callers take notice, goes first
+  bool roomy = true, few = true;
+  auto fits = [&](bool r, bool f) {
+    roomy = r;
+    few = f;
+    return bytes >= carve(g.eff, g, nullptr, nullptr, nullptr, r, f);
+  };
+  if (!fits(true, true) && !fits(true, false) && !fits(false, true) && !fits(false, false)) return MOE_ERR_WORKSPACE;
   moe_plan* p = new (std::nothrow) moe_plan();
   if (!p) return MOE_ERR_ARG;
   p->cfg = g.eff;
@@ -213,7 +220,7 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
   p->copy_in = p->copy_out = nullptr;
   p->submitted = 0;
   for (int b = 0; b < 2; ++b) p->ev_in[b] = p->ev_done[b] = p->ev_out[b] = nullptr;
-  carve(g.eff, g, (char*)d_workspace, &p->s, &p->counters_bytes, roomy);
+  carve(g.eff, g, (char*)d_workspace, &p->s, &p->counters_bytes, roomy, few);
   if (cudaGetDevice(&p->device) != cudaSuccess ||
       cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess) {
     delete p;
@@ -225,21 +232,13 @@ int moe_plan_create(const moe_config_t* cfg, void* d_workspace, size_t bytes, mo
       cudaMemset(p->s.ord_exit, 0, sizeof(int) * 2) != cudaSuccess ||
       cudaMemset(p->s.gemm1_done, 0, sizeof(int) * (size_t)(g.P + 4)) != cudaSuccess ||
       cudaMemset(p->s.clock_probe, 0, 2 * sizeof(unsigned long long)) != cudaSuccess ||
-      (p->s.few_sync && cudaMemset(p->s.few_sync, 0, sizeof(unsigned) * 96) != cudaSuccess)) {
+      // The one-launch layer's barriers count on from zero; its first call waits for this, and for what else used the memory before (few_start).
+      (p->s.few_sync && (cudaMemset(p->s.few_sync, 0, sizeof(unsigned) * kFewSync) != cudaSuccess ||
+                         cudaEventCreateWithFlags(&p->few_ready, cudaEventDisableTiming) != cudaSuccess ||
+                         cudaEventRecord(p->few_ready, cudaStreamLegacy) != cudaSuccess))) {
+    if (p->few_ready) cudaEventDestroy(p->few_ready);
     delete p;
     return MOE_ERR_CUDA;
-  }
-  if (p->s.few_sync) {
-    // The one-launch layer's barriers count on from what the memset leaves: it is waited for, since the first call may come on a stream
-    // that the default stream does not order.  (Not prohibited by a capture on another stream.)
-    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
-    cudaThreadExchangeStreamCaptureMode(&mode);
-    const cudaError_t e = cudaStreamSynchronize(0);
-    cudaThreadExchangeStreamCaptureMode(&mode);
-    if (e != cudaSuccess) {
-      delete p;
-      return MOE_ERR_CUDA;
-    }
   }
   *out = p;
   return MOE_OK;
@@ -254,6 +253,7 @@ int moe_plan_destroy(moe_plan_t* plan) {
       if (plan->ev_done[b]) cudaEventDestroy(plan->ev_done[b]);
       if (plan->ev_out[b]) cudaEventDestroy(plan->ev_out[b]);
     }
+    if (plan->few_ready) cudaEventDestroy(plan->few_ready);
     if (plan->copy_in) cudaStreamDestroy(plan->copy_in);
     if (plan->copy_out) cudaStreamDestroy(plan->copy_out);
   }

@@ -22,7 +22,7 @@ enum WaitSite { kWaitTileTable = 1, kWaitMbarTma = 3, kWaitMbarMma = 4,
                 kWaitMbarEpi = 5, kWaitMbarTmemFree = 6, kWaitTileReady = 7, kWaitItem = 8,
                 kWaitGrid = 9 };
 
-constexpr int kFewPartial = 16384;
+constexpr int kFewPartial = 16384, kFewSync = 96;
 struct Scratch {          // device pointers carved out of the caller's workspace
   int* status;            // [4]
   int* pool_next;         // [1]   paged mode: next free tile
@@ -46,8 +46,8 @@ struct Scratch {          // device pointers carved out of the caller's workspac
   unsigned char* group_large;  // [P*8] with recv_planes: which groups of 16 rows hold large numbers
   float* route_logits;    // [T, 256] router logits, more than 64 experts: the chain kernel's, or the tensor-core filter's approximate ones
   int route_slices;       // the slices of h that they are in (route_direct_kernel's: [route_slices, T, 256]); 0: another router
-  float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens; else nullptr)
-  unsigned* few_sync;     // [96]  its three grid barriers (every launch flips their highest bits)
+  float* few_logits;      // [256, T] the one-launch layer's router logits (up to MOE_FEW_MAX_TOKENS tokens, where the workspace has room; else nullptr)
+  unsigned* few_sync;     // [kFewSync]  its three grid barriers (every launch flips their highest bits)
   float* few_partial;     // [2 * H + kFewPartial, T] and its outputs in parts (a CTA of at most 256 has no less than half of another's units, so that
                           // up to 2 * 256 / (H / 32) + 2 have some of 32 rows)
   float* route_wnorm2;    // [256]    squared norms of the router's weight rows, recomputed by every call (filter)
@@ -111,6 +111,7 @@ struct moe_plan {
   int cuda_error;            // last CUDA error a call of this plan met (cudaError_t), 0 if none
   int cuda_error_step;       // which step of moe_layer met it: 1 router, 2 dispatch, 3 experts, 4 combine
   int timing;                // moe_layer_timed: record an event after every kernel of the layer
+  cudaEvent_t few_ready;     // few_sync is cleared; nullptr once the one-launch layer's first call has taken notice (or without few_sync)
   int trace;                 // moe_availability_trace: the dispatch kernels write avail_ns
   cudaEvent_t tev[MOE_STAGE_COUNT + 1];
 };

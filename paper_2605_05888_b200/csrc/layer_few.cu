@@ -445,6 +445,27 @@ static bool split_outputs(const moe_plan* p, int group) {
   return 2.0 * us * (alone / shared - 1.0) > 4.5;
 }
 
+// A plan's first launch is ordered behind what plan creation did on the default stream, which the call's own stream may not follow: on the
+// device, or where that is being captured on the host (a graph cannot wait for what is not part of it; the mode allows a wait in a capture).
+static cudaError_t few_start(moe_plan* p, cudaStream_t st) {
+  if (p->few_ready == nullptr) return cudaSuccess;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  cudaError_t e = cudaStreamIsCapturing(st, &capture);
+  if (e != cudaSuccess) return e;
+  if (capture == cudaStreamCaptureStatusNone) {
+    e = cudaStreamWaitEvent(st, p->few_ready, 0);
+  } else {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    e = cudaEventSynchronize(p->few_ready);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+  }
+  if (e != cudaSuccess) return e;
+  cudaEventDestroy(p->few_ready);  // (what waits for it does so all the same)
+  p->few_ready = nullptr;
+  return cudaSuccess;
+}
+
 // The checks and the launch that both entry points share.
 static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bias, LfMatrix wg, LfMatrix wu, LfMatrix wd, int group,
                      void* y, cudaStream_t st) {
@@ -459,6 +480,7 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
                ? MOE_OK
                : MOE_ERR_CUDA;
   }
+  if (p->s.few_sync == nullptr) return MOE_ERR_WORKSPACE;
   // numbers of units and of rows are 32-bit
   const long long eb = c.dtype == MOE_DTYPE_BF16 ? 2 : 4, entries = min(2ll * p->route_E, (long long)c.T * p->route_K);
   if ((long long)c.T * c.H * eb >= 1ll << 31 || entries * kLfSlots * c.F * p->tp * eb >= 1ll << 31 || p->sm_count > 256) return MOE_ERR_UNSUPPORTED;
@@ -493,11 +515,13 @@ static int layer_few(moe_plan* p, const void* x, const void* wr, const float* bi
   q.status = p->s.status;
   q.wait_ns = c.wait_limit_ns ? c.wait_limit_ns : kDefaultWaitNs;
   const bool small = reading_us(p, group) < kSmallUs;
-  cudaError_t e = group == 32    ? (small ? launch_cooperative<W4<32, true>>(p, q, st) : launch_cooperative<W4<32, false>>(p, q, st))
-                  : group == 64  ? (small ? launch_cooperative<W4<64, true>>(p, q, st) : launch_cooperative<W4<64, false>>(p, q, st))
-                  : group == 128 ? (small ? launch_cooperative<W4<128, true>>(p, q, st) : launch_cooperative<W4<128, false>>(p, q, st))
-                  : c.dtype != MOE_DTYPE_BF16 ? launch_cooperative<float>(p, q, st)
-                  : q.T > 4 && q.T * q.K >= 2 * q.E ? launch_cooperative<__nv_bfloat16, 2>(p, q, st) : launch_cooperative<__nv_bfloat16>(p, q, st);
+  cudaError_t e = few_start(p, st);
+  if (e == cudaSuccess)
+    e = group == 32    ? (small ? launch_cooperative<W4<32, true>>(p, q, st) : launch_cooperative<W4<32, false>>(p, q, st))
+        : group == 64  ? (small ? launch_cooperative<W4<64, true>>(p, q, st) : launch_cooperative<W4<64, false>>(p, q, st))
+        : group == 128 ? (small ? launch_cooperative<W4<128, true>>(p, q, st) : launch_cooperative<W4<128, false>>(p, q, st))
+        : c.dtype != MOE_DTYPE_BF16 ? launch_cooperative<float>(p, q, st)
+        : q.T > 4 && q.T * q.K >= 2 * q.E ? launch_cooperative<__nv_bfloat16, 2>(p, q, st) : launch_cooperative<__nv_bfloat16>(p, q, st);
   if (e != cudaSuccess) {
     cudaGetLastError();
     p->cuda_error = (int)e;

@@ -1,4 +1,6 @@
 """The MoE layer for a few tokens in one launch, on bf16, fp32 and 4-bit experts, against its definition in 64 bits."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -339,6 +341,83 @@ def test_plan_made_behind_other_work_and_first_called_on_a_stream_of_its_own():
         s.call(y=y, plan=plan, stream=here)
         here.synchronize()
         assert plan.moe_last_status() == (0, 0) and torch.equal(y, want)
+
+
+def plan_on(room, cfg, nbytes):
+    """A plan on given memory (a Plan takes as much as it may), or the library's refusal."""
+    plan = B.Plan.__new__(B.Plan)
+    plan.cfg, plan.device, plan.P, plan.workspace, plan.handle = cfg, room.device, B.moe_pool_tiles(cfg), room, ctypes.c_void_p()
+    rc = B.lib().moe_plan_create(ctypes.byref(cfg), room.data_ptr(), nbytes, ctypes.byref(plan.handle))
+    return plan if rc == 0 else rc
+
+
+@pytest.mark.parametrize("T,dtype", [(1, BF16), (16, BF16), (7, FP32)])
+def test_workspace_without_room_for_the_one_launch_layer(T, dtype):
+    """A workspace without what this layer alone needs is enough for every other call."""
+    s = Layer(T, 264, 8, 2, 136, dtype=dtype)
+    want, full = torch.empty_like(s.y), B.moe_workspace_bytes(s.plan.cfg)
+    s.plan.moe_layer(s.x, s.wr, None, *s.w, want)
+    saved = T * (8 * 264 + 66560) + 512
+    lean = full - saved
+    room = torch.empty(full, dtype=torch.uint8, device="cuda")
+    for nbytes, few in ((lean, False), (full - 1, False), (full, True)):
+        room.fill_(0xff)
+        plan = plan_on(room, s.plan.cfg, nbytes)
+        for _ in range(2):
+            s.y.zero_()
+            plan.moe_layer(s.x, s.wr, None, *s.w, s.y)
+            assert torch.equal(s.y, want) and plan.moe_last_status() == (0, 0)
+            if few:
+                assert torch.equal(s.call(plan=plan).clone(), s.call())
+                continue
+            s.y.fill_(7.0)
+            with pytest.raises(B.MoeError) as err:
+                s.call(plan=plan)
+            assert err.value.code == -7 and (s.y == 7.0).all()
+        assert (room[nbytes:] == 0xff).all()
+        plan.close()
+    assert plan_on(room, s.plan.cfg, lean - 256) == -7
+
+
+def test_plan_creation_waits_for_nothing():
+    s = Layer(2, 512, 8, 2, 256)
+    room = torch.empty(B.moe_workspace_bytes(s.plan.cfg), dtype=torch.uint8, device="cuda")
+    big = torch.randn(8192, 8192, device="cuda")
+    big @ big
+    done = torch.cuda.Event()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big @ big
+    done.record()
+    plan = plan_on(room, s.plan.cfg, room.numel())
+    assert not done.query()                               # (a tenth of a second of work)
+    y = torch.zeros_like(s.y)
+    assert torch.equal(s.call(plan=plan, y=y), s.call())
+
+
+def test_first_call_captured_and_never_replayed_or_replayed_in_between():
+    """Whatever the workspace held, and whichever of a graph and a plain call runs first: both find the barriers' start."""
+    s = Layer(4, 512, 8, 2, 256, seed=6)
+    want = s.call().clone()
+    for fill in (0x7f, 0xff):
+        for replays in (0, 1, 3):
+            room = torch.full((B.moe_workspace_bytes(s.plan.cfg),), fill, dtype=torch.uint8, device="cuda")
+            plan = plan_on(room, s.plan.cfg, room.numel())
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            y = torch.zeros_like(want)
+            with torch.cuda.graph(graph):
+                s.call(plan=plan, y=y)
+                s.call(plan=plan, y=y)
+            for _ in range(replays):
+                y.zero_()
+                graph.replay()
+                assert torch.equal(y, want) and plan.moe_last_status() == (0, 0)
+            for _ in range(3):
+                for run in (lambda: s.call(plan=plan, y=y), lambda: s.call(plan=plan, y=y), graph.replay):
+                    y.zero_()
+                    run()
+                    assert torch.equal(y, want) and plan.moe_last_status() == (0, 0)
 
 
 def test_gate_results_that_only_fp32_holds():
