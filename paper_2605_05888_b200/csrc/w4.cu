@@ -227,10 +227,11 @@ static int sm_count_now() {
   return sms;
 }
 
-// The grid, and the lanes of a row's segment (at least a group's).
+// The grid, and the lanes of a row's segment: at least a group's, up to a warp's, more where a row would have more segments than a grid's
+// second dimension may count (rows of 2^25 columns).
 static dim3 pack_grid(PackShape& p, int group, int unroll) {
   p.lanes = group / 8;
-  while (p.lanes < 32 && p.lanes < p.C / 8) p.lanes *= 2;
+  while ((p.lanes < 32 && p.lanes < p.C / 8) || (p.lanes < kPackThreads && p.C / 8 > 65535 * p.lanes * unroll)) p.lanes *= 2;
   const int rows = kPackThreads / p.lanes, words = p.lanes * unroll;
   return dim3((p.N + rows - 1) / rows, (p.C / 8 + words - 1) / words, p.experts < 65535 ? p.experts : 65535);
 }

@@ -141,6 +141,44 @@ def test_pack_of_more_rows_than_the_grid(dtype, E, N, C, group):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,C,group", [(1, 1 << 25, 128), (3, (1 << 25) - 32, 32), (2, 65535 * 512 + 64, 64), (2, 65535 * 512, 128)])
+def test_pack_of_the_longest_rows(dtype, N, C, group):
+    """The most columns that the calls take, and both sides of what 65535 segments of 512 columns hold."""
+    g = torch.Generator(device="cuda").manual_seed(7)
+    w = torch.empty(1, N, C, dtype=dtype, device="cuda").normal_(0.0, 0.02, generator=g)
+    out = B.W4(torch.full((1, N, C // 2), 0xa5, dtype=torch.uint8, device="cuda"), torch.full((1, C // group, N), 123.0, dtype=torch.bfloat16, device="cuda"))
+    B.moe_w4_pack(w, out)
+    groups = w.view(N, C // group, group)
+    scales = (groups.abs().amax(-1).double() / 7).float().to(torch.bfloat16)    # (53 bits are enough: the quotient rounds to fp32 as the exact one)
+    assert torch.equal(out.scales[0], scales.T)
+    back = torch.empty_like(w)
+    B.moe_w4_unpack(out, back)
+    for n in range(N):
+        s = scales[n].double().unsqueeze(-1)
+        want = (torch.round(groups[n].double() / s).clamp(-8, 7) * s).flatten()
+        assert torch.equal(back[0, n], want.float().to(dtype))
+
+
+@gpu
+def test_matvec_of_the_longest_rows():
+    N, C, group = 3, 1 << 25, 128
+    g = torch.Generator(device="cuda").manual_seed(8)
+    codes = torch.randint(0, 256, (N, C // 2), dtype=torch.uint8, device="cuda", generator=g)
+    scales = torch.empty(C // group, N, dtype=torch.bfloat16, device="cuda").uniform_(0.5, 1.5, generator=g)
+    x = torch.zeros(2, C, dtype=torch.bfloat16, device="cuda")     # few columns that count, so that the sums' roundings stay small
+    at = torch.randint(0, C, (500,), device="cuda", generator=g)
+    at[:2] = torch.tensor([0, C - 1], device="cuda")
+    x[:, at] = torch.empty(2, 500, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    y = torch.empty(2, N, dtype=torch.bfloat16, device="cuda")
+    B.moe_w4_matvec(B.W4(codes, scales), x, None, y)
+    # a sum's rounding is in proportion to what it has come to: the additions of zeros add none, so the bound counts the 500
+    at = at.unique()
+    want, bound = R.matvec(torch.stack([R.weights(codes[n:n + 1], scales[:, n:n + 1])[0, at] for n in range(N)]), x[:, at].double())
+    R.assert_within(y, want, bound + R.HALF[torch.bfloat16] * (want.abs() + bound), "y")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_pack_on_the_borders_between_codes(dtype):
     """Weights at (k + 1/2) s and one step of their type on either side of it, for scales of every mantissa."""
     rows = []
