@@ -118,6 +118,23 @@ def test_much_4bit_work_and_ragged_rows(T, H, E, K, F, group):
     Layer(T, H, E, K, F, group=group, renorm=T % 2, bias=True, seed=T + group).check()
 
 
+@pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])
+def test_root_mean_square_error_of_long_sums(dtype, group):
+    """The bounds per value grow with the sums' lengths; the error over all values holds sums of thousands of terms to what one left out would show
+    (1 / sqrt(H) of gate or up, 1 / sqrt(K F) of down: 0.02 and 0.01 here)."""
+    T, H, E, K, F = 16, 2048, 4, 2, 4096
+    s = Layer(T, H, E, K, F, dtype=dtype, group=group, renorm=1, seed=21)
+    got = s.call().double()
+    idx = s.plan.layer_tensor(0).long()
+    want = R.layer(s.x.double(), s.wr.double(), None, s.matrix(0), s.matrix(1), s.matrix(2), K, 1, idx, dtype)[3]
+    # n roundings of at most 2^-23 of a partial sum, whose root mean square is at most the whole sum's, are n 2^-23 of it together (Minkowski):
+    # a matrix instruction of sixteen columns cuts off seventeen addends; silu(g) u takes g's error by silu' <= 1.1 where silu is half of g or more,
+    # and u's; the tokens' two numbers double the down product's; 1e-5 for the weights and for what the second numbers leave.
+    sums = (3.2 * H + 2 * F) * 17 / 16 * R.U32 + 1e-5
+    # the final rounding: uniform within half a step, at most HALF / sqrt(3) of a value; 2 % for the sample
+    assert (got - want).norm() / want.norm() <= R.HALF[dtype] / 3 ** 0.5 * 1.02 + sums < 0.005
+
+
 def kinds(f):
     return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
 
@@ -443,6 +460,27 @@ def test_wait_that_runs_out_is_reported():
     s.call()
     assert s.plan.moe_last_status()[0] == code
     Layer(2, 512, 8, 2, 256).check()
+
+
+@pytest.mark.parametrize("kw,barriers", [(dict(T=2, H=512, E=8, K=2, F=256), 2), (dict(T=16, H=36, E=16, K=4, F=8192, dtype=FP32), 3)])
+def test_barriers_count_right_after_waits_that_ran_out(kw, barriers):
+    """Every launch adds 2^31 to each of its barriers' counters, whether or not a wait in it ran out.  Two equal calls leave the same workspace but
+    for the counters, which is how they are found."""
+    s = Layer(**kw, seed=3)
+    words = lambda plan: plan.workspace[:plan.workspace.numel() // 4 * 4].view(torch.int32)  # noqa: E731
+    s.call()
+    before = words(s.plan).clone()
+    s.call()
+    at = (words(s.plan) != before).nonzero().flatten()
+    assert at.numel() == barriers and (words(s.plan)[at] ^ before[at] == -2 ** 31).all()
+    plan = B.Plan(B.make_config(s.T, s.H, s.E, 1, s.K, s.F, s.plan.cfg.dtype, wait_limit_ns=1))
+    assert plan.workspace.numel() == s.plan.workspace.numel() and plan.workspace.data_ptr() % 256 == s.plan.workspace.data_ptr() % 256 == 0
+    late = 0
+    for n in range(1, 9):
+        s.call(plan=plan)
+        late += plan.moe_last_status() != (0, 0)
+        assert (words(plan)[at] == (-2 ** 31 if n % 2 else 0)).all(), n
+    assert late > 0
 
 
 def test_empty_batch():

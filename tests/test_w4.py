@@ -258,6 +258,24 @@ def test_matvec_long_columns_of_few_rows():
 
 
 @gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M", [8, 16])
+def test_matvec_root_mean_square_error_of_long_rows(group, M):
+    """A column left out of 7168 would be 0.012 of a result; the bound per value alone would not show it."""
+    N, C = 3000, 7168
+    g = torch.Generator(device="cuda").manual_seed(group + M)
+    codes, scales = R.random_w4(g, 0.05, N, C, group=group)
+    x = torch.empty(M, C, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    B.moe_w4_matvec(B.W4(codes, scales), x, None, y)
+    want = x.double() @ R.weights(codes, scales).T
+    # (seventeen addends cut off per matrix instruction of sixteen columns, a rounding per group, each of a partial sum that is no larger than the whole
+    # in the root mean square; the final rounding, uniform within half a step, and 2 % for the sample)
+    bound = R.HALF[torch.bfloat16] / 3 ** 0.5 * 1.02 + (C * 17 / 16 + C / group) * R.U32
+    assert (y.double() - want).norm() / want.norm() <= bound < 0.004
+
+
+@gpu
 def test_matvec_codes_beyond_four_gigabytes():
     E, N, C, group = 140, 8192, 8192, 128
     assert E * N * C // 2 > 2 ** 32
