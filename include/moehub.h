@@ -393,7 +393,7 @@ int moe_layer_few_w4(moe_plan_t* plan, const void* d_x, const void* d_wr, const 
  * A row whose id is outside [0, experts) is skipped: its y keeps its old contents.  One matrix is read once for every 8 rows (M <= 8)
  * or 16; of several, rows with the same one share its reading by eights as far as they are among the same 32 consecutive rows.  M may be
  * any number up to 2^30 (with hundreds of rows moe_w4_unpack and a matrix product are the better way), experts up to 65535, N up to 2^25
- * (MOE_ERR_UNSUPPORTED beyond).  y is not x.  Needs no plan and no workspace; runs on the current device. */
+ * (MOE_ERR_UNSUPPORTED beyond).  y is not x (MOE_ERR_ARG).  Needs no plan and no workspace; runs on the current device. */
 int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const moe_w4_t* w, int32_t M, const void* d_x,
                   const int32_t* d_expert, void* d_y, void* stream);
 

@@ -384,6 +384,7 @@ int moe_w4_matvec(int32_t experts, int32_t N, int32_t C, int32_t group, const mo
   if (experts > 65535 || N > (1 << 25) || M > (1 << 30)) return MOE_ERR_UNSUPPORTED;  // (matrix numbers are held in 16 bits, numbers of rows in 32)
   if (((reinterpret_cast<uintptr_t>(d_x) | reinterpret_cast<uintptr_t>(d_y)) & 15) || (reinterpret_cast<uintptr_t>(d_expert) & 3))
     return MOE_ERR_ALIGN;
+  if (d_x == d_y) return MOE_ERR_ARG;  // (rows are read while others' results are written)
   const W4MatvecParams q{w->codes, (const __nv_bfloat16*)w->scales, (const __nv_bfloat16*)d_x, d_expert, (__nv_bfloat16*)d_y, experts, N, C, M};
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = group == 32 ? launch_matvec<32>(q, st) : group == 64 ? launch_matvec<64>(q, st) : launch_matvec<128>(q, st);

@@ -57,6 +57,14 @@ def test_calls_refuse_what_they_cannot_take(lib):
         assert call(w=a + 4) == call(out=B.W4T(a + 4, a)) == -2
 
 
+def test_product_in_the_place_of_its_rows_is_refused(lib):
+    """Other threads' rows are still being read when the first results are written."""
+    a = 1 << 20
+    for M in (1, 3, 17):
+        for experts, ids in ((1, None), (4, a)):
+            assert lib.moe_w4_matvec(experts, 128, 128, 32, ctypes.byref(B.W4T(a, a)), M, a, ids, a, None) == -1
+
+
 def test_matrices_that_do_not_belong_together_are_refused():
     u8, bf = torch.uint8, torch.bfloat16
     w = B.W4(torch.zeros(3, 5, 64, dtype=u8), torch.zeros(3, 4, 5, dtype=bf))
