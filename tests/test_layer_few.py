@@ -135,6 +135,28 @@ def test_root_mean_square_error_of_long_sums(dtype, group):
     assert (got - want).norm() / want.norm() <= R.HALF[dtype] / 3 ** 0.5 * 1.02 + sums < 0.005
 
 
+def test_long_bf16_sums_keep_the_accuracy_of_fp32():
+    """65536 terms that cancel: what is left of a gate product is its sum's error, and the layer's weights put it into y.  Matrix instructions cut
+    off, towards zero, so a sum that goes through a chain of them loses a part of itself with each: such chains end with a chunk of 64 columns."""
+    H, F = 65536, 148 * 128                                    # (whole tiles for every warp: nothing else cuts the sums)
+    s = Layer(1, 8, 1, 1, 8, seed=2)
+    half = torch.empty(H // 2, dtype=BF16, device="cuda").uniform_(0.5, 1.0).mul_(2.0 ** -10)
+    tokens = torch.empty(H // 2, dtype=BF16, device="cuda").uniform_(0.5, 1.0)
+    tokens[0] = 1.0
+    gate, s.x = torch.cat([half, -half.flip(0)]), torch.cat([tokens, tokens.flip(0)]).view(1, H)
+    s.wr = torch.zeros(1, H, dtype=BF16, device="cuda")
+    s.w = [gate.expand(1, F, H).contiguous(), torch.zeros(1, F, H, dtype=BF16, device="cuda"), torch.zeros(1, H, F, dtype=BF16, device="cuda")]
+    s.w[1][0, :, 0] = 2.0                                      # silu(g) 2 is g where g is small
+    s.w[2][0, :F].fill_diagonal_(1.0)
+    y = s.call(plan=B.Plan(B.make_config(1, H, 1, 1, 1, F, B.DTYPE_BF16)), y=torch.empty(1, H, dtype=BF16, device="cuda"))
+    # M: the largest partial sum, reached linearly.  1024 additions of chunks, each rounded to half a step of a sum of M / 2 on average; in each chunk
+    # four instructions that cut off seventeen addends, each by a step of at most the chunk's sum of M / 512: 512 + 272 times 2^-24 M.  2 % for silu
+    # and the roundings to bf16.
+    M = (half.double() * tokens.double()).sum().item()
+    assert y[0, :F].double().abs().max().item() <= 1.02 * (512 + 272) * 2.0 ** -24 * M
+    assert (y[0, F:] == 0).all()
+
+
 def kinds(f):
     return pytest.mark.parametrize("dtype,group", [(BF16, 0), (FP32, 0), (BF16, 32), (BF16, 128)])(f)
 
