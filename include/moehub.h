@@ -356,7 +356,8 @@ int moe_layer(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* 
  * configuration T, H, E, K, F, dtype, renormalize and wait_limit_ns count (tp_shards changes nothing: an expert is computed
  * whole), identity experts are refused (MOE_ERR_ARG).  It differs from moe_layer in its rounding.  Logits are fp32 sums in an
  * order of their own, not the ascending chain of moe_route: the pick between two experts whose logits agree to fp32 rounding
- * may differ.  The SwiGLU results and the experts' outputs are not rounded to bf16 on the way; only y is.
+ * may differ.  The SwiGLU results are held to 2^-17 of a value on the way (as two bf16 numbers; dtype fp32:
+ * as fp32 numbers), the experts' outputs as fp32 sums; only y is rounded to bf16.
  * The result does not depend on the order in which the CTAs run, but a token's last bits may depend on which experts the other
  * tokens of the batch pick (the reading of the weights, and so the order of a sum, is shared out anew).
  * moe_layer_buffer 0, 1 and 3 (picks, their weights, rows per expert) hold the call's values behind it, the other buffers
@@ -384,7 +385,8 @@ typedef struct {
 /* moe_layer_few with 4-bit expert weights: wg, wu as [E] matrices [F, H], wd as [E] matrices [H, F], one group size for the three.
  * (The structs are read before the call returns.)  x, the router weight and y are bf16 (a plan of dtype fp32 is refused with
  * MOE_ERR_UNSUPPORTED, so is another group size; MOE_ERR_ARG where the group does not divide H and F).  Products are formed with the
- * exact integers code - 8 and summed in fp32, a group's sum is scaled once. */
+ * exact integers code - 8 and summed in fp32, a group's sum is scaled once (so a token or a SwiGLU result times 8 * group has to be an
+ * fp32 number; in moe_w4_matvec too). */
 int moe_layer_few_w4(moe_plan_t* plan, const void* d_x, const void* d_wr, const float* d_bias, int32_t group,
                      const moe_w4_t* wg, const moe_w4_t* wu, const moe_w4_t* wd, void* d_y, void* stream);
 

@@ -12,11 +12,13 @@
 //
 // Bound by reading the picked experts' weights once; for one token of small experts by latencies, which the trace of one Qwen-like token shows,
 // us: launch and router 2.4, barrier 1.2 of it, selection 2, gate/up 7 (46 MB), joins 1, the others' arrival and the barrier 3, down 4 (23 MB), end 1.
-// Measured, device time, us, moe_layer (three launches or more) / this / the picked experts' bytes at the copy rate.  bf16: Qwen-like 1 token
-// 27.6 / 21.7 / 10.5, 16 tokens 130 / 118 / 104; Mixtral-like 1 token 124 / 114 / 107, 5 tokens 379 / 340 / 340, 16 tokens 470 / 427 / 429;
-// DeepSeek-like 1 token 145 / 116 / 107, 16 tokens 1302 / 1223 / 1252; of 8 experts of 512 x 512, 4 tokens, 14.2 / 14.8 / 1.4 (latencies
-// alone).  fp32, 16 experts of 1020 x 2044, 3 tokens: 107 / 38 / 23.  4 bits (this / bytes): Qwen-like 1 token 18.3 / 2.8, Mixtral-like 7 tokens
-// 170 / 116, DeepSeek-like 16 tokens 522 / 350: bound by the instructions that unpack the codes (row_stream.cuh).
+// Measured, device time by graph replay, us, moe_layer (three launches or more) / this / the picked experts' bytes at the copy rate (which a stream
+// that only reads can beat by some per cent).  bf16: Qwen-like 1 token 27.4 / 21.8 / 10.5, 16 tokens 129 / 118 / 104; Mixtral-like 1 token
+// 123 / 111 / 107, 5 tokens 378 / 335 / 340, 16 tokens 462 / 430 / 429; DeepSeek-like 1 token 145 / 114 / 107, 16 tokens 1279 / 1193 / 1252; of 8
+// experts of 512 x 512, 4 tokens, 13.8 / 14.1 / 1.4 (latencies alone).  fp32: 16 experts of 1020 x 2044, 3 tokens, 105 / 37 / 23; Phi-like 8 tokens
+// 724 / 487 / 479.  4 bits (this / expected bytes), groups of 128: Qwen-like 1 token 18.1 / 2.8, Mixtral-like 1 token 57 / 28, 7 tokens 171 / 95 (all
+// eight experts: 116), DeepSeek-like 16 tokens 525 / 350; groups of 64 and 32: Mixtral-like 7 tokens 182 / 98 and 203 / 104.  No unit and not HBM is full
+// there: instructions that unpack the codes, and their latencies (row_stream.cuh).
 #include "route_common.cuh"
 #include "row_stream.cuh"
 
@@ -306,8 +308,8 @@ __device__ __forceinline__ float lf_silu_mul(float g, float u) { return g / (1.0
 
 // DOWN: eights of token slots in the down product's entries, so that these have up to 4 * DOWN tokens as two numbers each.  2 where an expert
 // has at least two of more than four tokens on average (launch below): its entries of more than four tokens else read its down rows twice,
-// the second time from L2.  Measured, us, 1 / 2: Mixtral-like 16 tokens 476 / 427, 11 tokens 435 / 424, 8 tokens 402 / 404, 6 tokens 384 / 385,
-// Phi-like 16 tokens 330 / 324, 8 tokens 243.7 / 244.1, Qwen-like 6 tokens 66.7 / 68.1.
+// the second time from L2.  Measured, us, 1 / 2: Mixtral-like 16 tokens 477 / 429, 11 tokens 435 / 427, 8 tokens 403 / 406, 6 tokens 387 / 389,
+// Phi-like 16 tokens 331 / 326, 8 tokens 242.6 / 244.4, Qwen-like 6 tokens 65.9 / 67.4.
 template <typename W, int DOWN>
 __global__ void __launch_bounds__(RsSizes<W, 1>::THREADS, 1)
 layer_few_kernel(const __grid_constant__ LayerFewParams p) {
@@ -421,24 +423,24 @@ static double reading_us(const moe_plan* p, int group) {
   const double bits = group > 0 ? 4.0 + 16.0 / group : c.dtype == MOE_DTYPE_BF16 ? 16.0 : 32.0;
   return (double)min(c.T * p->route_K, p->route_E) * c.H * c.F * p->tp * bits / 8.0 / 6.0e6;
 }
-// (4 bits) Below this the small form of the code.  Measured, us, small / other: Qwen-like 1 token 18.6 / 20.0, 4 tokens (4 us of reading) 35.4 / 39.3,
-// 16 tokens (15 us) 65.9 / 66.2, 16 tokens of 64 experts of 1024 x 1024 (6 us) 46.6 / 48.5, Mixtral-like 1 token (10 us) 62.1 / 62.0, 7 tokens (40 us)
-// 178.6 / 169.8, DeepSeek-like 1 token (10 us) 65.9 / 62.6, 4 tokens (40 us) 187 / 179, 16 tokens 552 / 523.
+// (4 bits) Below this the small form of the code.  Measured, us, small / other: Qwen-like 1 token 18.4 / 19.8, 4 tokens (4 us of reading) 35.6 / 39.4,
+// 16 tokens (15 us) 66.7 / 67.6, 16 tokens of 64 experts of 1024 x 1024, top-4 (6 us) 41.0 / 39.8, Mixtral-like 1 token (10 us) 60.3 / 57.8, 7 tokens (40 us)
+// 181 / 171, DeepSeek-like 1 token (10 us) 67.7 / 63.8, 4 tokens (40 us) 189 / 179, 16 tokens 559 / 547.
 constexpr double kSmallUs = 9.0;
 
 // Whether all CTAs share all outputs' terms, which costs a third barrier and the joining of the parts, 3 to 4 us, and saves what a CTA with
 // rows of its own loses: with 4 bits, which are bound by instructions, to the rows that its sixteens lack (48.4 rows take as long as 64) and to
-// warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured before the
-// loop over 4-bit rows took its present form, whole layers, us, rows of its own / shared.  4 bits: DeepSeek-like 1 token 71.1 / 74.5, 2 tokens 114.6 / 114.8, 4 tokens 205 / 193, 16 tokens 622 / 560; Mixtral-like
-// 1 token 71.8 / 74.6, 7 tokens 190 / 186; Qwen-like 4 tokens 39.5 / 41.1, 16 tokens 78.8 / 73.7.  16 tokens, 64 experts of 1024 x 1024: 4 bits
-// 64 / 54, bf16 77 / 63, fp32 158 / 120; 1 token, 16 of 1024 x 2048: bf16 14.9 / 15.8, fp32 22.9 / 23.7, 3 tokens 25.8 / 26.7 and 40.6 / 38.6.
+// warps' last units; else, where it has fewer than sixteen rows, to loops over many columns that are bound by latencies.  Measured, whole
+// layers, us, rows of its own / shared.  4 bits: DeepSeek-like 1 token 63.7 / 66.5, 2 tokens 105.8 / 105.1, 4 tokens 189 / 179, 16 tokens 583 / 529; Mixtral-like
+// 1 token 57.8 / 62.0, 7 tokens 174 / 171; Qwen-like 1 token 18.4 / 21.5, 4 tokens 35.8 / 38.2, 16 tokens 78.5 / 66.8.  16 tokens, 64 experts of 1024 x 1024,
+// top-4: 4 bits 47 / 41, bf16 69 / 57, fp32 137 / 101; 1 token, 16 of 1024 x 2048: bf16 15.2 / 16.0, fp32 21.2 / 21.8, 3 tokens 26.4 / 26.6 and 40.7 / 34.6.
 static bool split_outputs(const moe_plan* p, int group) {
   const moe_config_t& c = p->cfg;
   const int G = p->sm_count, picked = min(c.T * p->route_K, p->route_E), F = c.F * p->tp, all_tiles = (c.H + kRsTile - 1) / kRsTile;
   if ((long long)all_tiles * kLfDownEntries * ((F + 31) / 32) >= 1ll << 31) return false;  // (numbers of units)
   const double us = reading_us(p, group);
   if (group == 0) return us * ((double)G * kRsRun / c.H - 1.0) > 4.5;
-  // a warp's units of sixteen rows, alone and shared; the multiplication takes about twice as long as the reading
+  // a warp's units of sixteen rows, alone and shared; the multiplication is taken to last twice as long as the reading (1.5 to 2 times)
   const int rows = (c.H + G - 1) / G, tiles = (rows + kRsTile - 1) / kRsTile, runs = (rows + tiles - 1) / tiles > kRsRun || us >= kSmallUs ? 2 : 1;
   const long long units = (long long)picked * ((F + RsFormat<W4<32, false>>::COLS - 1) / RsFormat<W4<32, false>>::COLS), warps = RsFormat<W4<32, false>>::WARPS;
   const double alone = (double)((tiles * units + warps - 1) / warps * runs), shared = (double)((all_tiles * units + warps * G - 1) / (warps * G) * 2);

@@ -64,9 +64,10 @@ template <int G, bool S> struct RsFormat<W4<G, S>> {
   typedef __nv_bfloat16 X;
   static constexpr bool SMALL = S;
   static constexpr int COLS = 256, GROUP = G, GROUPS = COLS / G;
-  // Bound by the instructions that unpack the codes (12 of about 19 per word, with the MMA) and by their latencies: the more warps the better, as long as
-  // their registers suffice.  Mixtral-like layer of 7 tokens, us, 8 / 12 / 16 / 18 warps, before the loop was made smaller: 266 / 206 / 181 / 204 (170 now); of the 181, without unpacking
-  // 167, without the tokens' loads 166, without the scales 178, without all three 129 (116 for the bytes); 54 % of the issue slots, 51 % of the ALU.
+  // Of about 20 instructions per word of eight codes 12 unpack and multiply it (3 shifts, 4 masks, 4 subtractions, an MMA).  No unit is full (55 % of the issue
+  // slots, 55 % of the ALU, HBM at 48 %): latencies count, so the more warps the better, as long as their registers suffice (at 16 the layers' code for
+  // groups of 64 and 32 spills 44 and 16 bytes, that for 128 nothing).  Mixtral-like layer of 7 tokens, us, 8 / 12 / 16 warps: 234 / 186 / 170.  An earlier form of the loop
+  // took 181: without unpacking 167, without the tokens' loads 166, without the scales 178, without all three 129 (116 for the bytes).
   static constexpr int WARPS = 16;
 };
 template <typename W, int NT> struct RsSizes {   // NT: token slots, in eights

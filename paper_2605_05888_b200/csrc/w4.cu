@@ -8,9 +8,12 @@ namespace moehub {
 // A warp takes a segment of a row (rows of few words: several), some words of eight columns per lane in flight: rows,
 // segments and matrices are the grid's three dimensions, so that no place has to be divided out and small matrices fill the GPU.  Packing goes
 // on to rows further down, whose words are loaded while these are coded; the grid is cut to a few rounds of CTAs for it.
-// Measured on 8 matrices of 14336 x 4096, groups of 128, us: unpacking 187 (181 for the bytes at the copy rate: bound by HBM), packing bf16
-// 219 (181): bound by the instructions, about 100 per word (82 % of the issue slots; four words per lane in flight and no next ones 280; two,
-// and one round of CTAs 239, 8 rounds 227, 32 rounds 241; three CTAs per SM of 8 rounds 245, five 239; two buffers in turn instead of a copy 219).
+// Measured on 8 bf16 matrices of 14336 x 4096, us, groups of 128 / 64 / 32: unpacking 188 / 193 / 200 (180 / 181 / 183 for the bytes at the copy rate: bound by
+// HBM; the smaller the groups, the more scales of two bytes, a row's N apart), packing 218 / 219 / 234: bound by the instructions, about 100 per word (76 % of
+// the issue slots; earlier forms: four words per lane in flight and no next ones 280; two, and one round of CTAs 239, 8 rounds 227, 32 rounds 241;
+// three CTAs per SM of 8 rounds 245, five 239; two buffers in turn instead of a copy is the present one).  4 fp32 matrices of that size: unpacking
+// 214 / 218 / 223, packing 196 / 195 / 196 (162 / 162 / 163 for the bytes): packing has 156 bytes of spills and a word near a border in one of
+// twenty steps of a warp, which all its lanes wait for.
 constexpr int kPackThreads = 256;
 constexpr int kPackUnroll = 2, kUnpackUnroll = 4;  // words per lane
 constexpr int kPackCtas = 4, kPackRounds = 8;      // of the packing kernel on an SM
@@ -331,9 +334,10 @@ static cudaError_t launch_matvec(const W4MatvecParams& q, int device, int sms, c
 }
 
 // 16 rows of one matrix at a time (with eight warps, for the registers) where there are more than eight: groups of 128, 7168 x 7168, us, by
-// eights / by sixteens: 8 rows 12.6 / 16.6, 9 rows 22.4 / 16.9, 32 rows 44.0 / 31.7; of several matrices rows that share one are few (24 rows of 60
-// matrices of 2817 x 2048 27.0 / 33.9).  The small code where a CTA has no more than sixteen rows of the matrices: 1408 x 2048, small / other,
-// 5.2 / 5.6, 16 rows 6.5 / 7.0; 7168 x 7168 16 rows 20.8 / 19.6; 24 rows of 60 matrices 27.6 / 27.0.
+// eights / by sixteens: 8 rows 12.0 / 15.0, 9 rows 22.0 / 15.5, 32 rows 43.1 / 30.4, 48 rows 63.5 / 45.1 (4.1 for the bytes: every sixteen rows read and expand
+// them anew); of several matrices rows that share one are few (24 rows of 60 matrices of 2817 x 2048 26.8 / 32.3).  The small code where a CTA has no
+// more than sixteen rows of the matrices: 1408 x 2048, small / other, 4.9 / 5.3, 16 rows 6.1 / 6.5; 7168 x 7168 16 rows 19.0 / 18.1; 24 rows of 60
+// matrices 27.2 / 26.9.
 template <int G>
 static cudaError_t launch_matvec(const W4MatvecParams& q, cudaStream_t st) {
   int device = 0;
