@@ -261,6 +261,13 @@ def test_matvec_more_rows_of_a_matrix_than_share_its_reading(ids):
 
 
 @gpu
+@pytest.mark.parametrize("M", [1, 8, 11, 20, 40])
+def test_matvec_one_matrix_with_ids(M):
+    """One matrix and an id per row: rows with another id are skipped, whatever the rows' number makes of the batch."""
+    check_matvec(1, 150, 384, 64, M, [0 if m % 3 else (-1, 1, 0, 7)[m % 4] for m in range(M)], seed=M)
+
+
+@gpu
 def test_matvec_long_columns_of_few_rows():
     check_matvec(1, 3, 128 * 400, 128, 2, None)
 
